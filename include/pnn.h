@@ -73,7 +73,9 @@ enum {
   PNN_ERR_HIP = -6,         /* a HIP call failed */
   PNN_ERR_INDEX = -7,       /* sub-network / coarse block index out of range */
   PNN_ERR_ALIGN = -8,       /* a pointer violates the alignment rules above */
-  PNN_ERR_TOO_LARGE = -9    /* the problem exceeds the fixed scratch of an allocation-free entry point */
+  PNN_ERR_TOO_LARGE = -9,   /* the problem exceeds the fixed scratch of an allocation-free entry point
+                               (pnn_seq.h: what the kernels index) */
+  PNN_ERR_VALUE = -10       /* a scalar argument is out of its range */
 };
 
 typedef enum { PNN_F32 = 0, PNN_BF16 = 1 } pnn_dtype;

@@ -1976,7 +1976,8 @@ const char* pnn_status_string(pnn_status s) {
     case PNN_ERR_HIP: return "a HIP call failed";
     case PNN_ERR_INDEX: return "index out of range";
     case PNN_ERR_ALIGN: return "a pointer is not aligned as the interface requires";
-    case PNN_ERR_TOO_LARGE: return "the problem exceeds the fixed scratch of an allocation-free entry point";
+    case PNN_ERR_TOO_LARGE: return "the problem exceeds the fixed scratch of an allocation-free entry point, or what an operator indexes";
+    case PNN_ERR_VALUE: return "a scalar argument is out of its range";
     default: return "unknown status";
   }
 }

@@ -1,0 +1,84 @@
+// Internal declarations of the sequence operators (pnn_seq.h): launchers called by the entry points
+// (seq.hip) once the arguments are checked, and the sizes both sides use.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "pnn_seq.h"
+
+namespace pnn {
+
+inline int64_t cdiv64(int64_t a, int64_t b) { return (a + b - 1) / b; }
+inline int64_t round256(int64_t v) { return (v + 255) / 256 * 256; }
+
+// ---- embedding ----
+constexpr int EMB_DIGIT = 9;           // bits of a radix pass
+constexpr int EMB_BINS = 1 << EMB_DIGIT;
+constexpr int EMB_ITEMS = 2048;        // tokens of a sorting workgroup
+constexpr int EMB_DIRECT = 64;         // sorting workgroups up to which each sums the others' histograms itself
+constexpr int EMB_RUN = 32;            // sorted positions of a summing tile
+// tokens outside the table sort as key = vocab, behind all others
+inline int embed_passes(int64_t vocab) {
+  int bits = 0;
+  while (bits < 32 && (vocab >> bits) != 0) ++bits;
+  return (bits + EMB_DIGIT - 1) / EMB_DIGIT;
+}
+// Workspace of the gradient: keys and positions twice (the radix passes go from one to the other),
+// a histogram [workgroup][bin] for every pass, and the partial rows [tile][2][width] of runs that
+// cross tiles.
+struct EmbedWs {
+  int64_t key[2], pos[2], hist, total, part, bytes;
+  int64_t blocks, tiles;
+  int passes;
+};
+inline EmbedWs embed_ws(const pnn_embed_desc& d) {
+  EmbedWs w;
+  w.blocks = cdiv64(d.n, EMB_ITEMS);
+  w.tiles = cdiv64(d.n, EMB_RUN);
+  w.passes = embed_passes(d.vocab);
+  int64_t o = 0;
+  for (int i = 0; i < 2; ++i) {
+    w.key[i] = o;
+    o += round256(d.n * 4);
+    w.pos[i] = o;
+    o += round256(d.n * 4);
+  }
+  w.hist = o;
+  o += round256(w.passes * w.blocks * EMB_BINS * 4);
+  w.total = o;
+  o += EMB_BINS * 4;
+  w.part = o;
+  o += round256(w.tiles * 2 * d.width * 4);
+  w.bytes = o;
+  return w;
+}
+int launch_embed_fwd(const pnn_embed_desc& d, const void* table, const void* tokens, void* out, hipStream_t s);
+int launch_embed_bwd(const pnn_embed_desc& d, const void* dout, const void* tokens, float* dtable, int accumulate,
+                     void* ws, hipStream_t s);
+
+// ---- recurrence ----
+constexpr int SCAN_CHUNK = 16;         // steps from one kept state to the next
+struct ScanArgs {
+  const void *x, *gate;
+  const int32_t* lengths;
+  const float* h0;
+  void* h;
+  float* hT;
+  float* states;       // [batch][chunks][channels]: the state each chunk starts from
+  const void* dh;
+  const float* dhT;
+  void *dx, *dgate;
+  float* dh0;
+  void* ws;
+};
+inline int64_t scan_chunks(const pnn_scan_desc& d) { return cdiv64(d.length, SCAN_CHUNK); }
+inline int64_t scan_ws_bytes(const pnn_scan_desc&) { return 0; }
+int launch_scan_fwd(const pnn_scan_desc& d, const ScanArgs& a, hipStream_t s);
+int launch_scan_bwd(const pnn_scan_desc& d, const ScanArgs& a, hipStream_t s);
+
+// ---- distillation ----
+int launch_distill(const pnn_distill_desc& d, const void* logits, const int32_t* index, const void* teacher,
+                   const int32_t* labels, const float* weight, float* loss, void* dlogits, hipStream_t s);
+
+}  // namespace pnn
