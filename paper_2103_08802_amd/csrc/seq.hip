@@ -58,9 +58,10 @@ pnn_status scan_ok(const pnn_scan_desc* d) {
   if (d == nullptr) return PNN_ERR_NULL;
   if (!type_ok(d->dtype)) return PNN_ERR_DTYPE;
   if (d->batch < 0 || d->length < 0 || d->channels < 0) return PNN_ERR_SHAPE;
-  if (d->batch > MAX_COUNT || d->length > MAX_COUNT || d->channels > MAX_COUNT) return PNN_ERR_TOO_LARGE;
-  // the states are held densely, and a launch has a thread for every channel of the batch
-  if (d->batch * d->channels > MAX_COUNT || d->batch * d->channels * (d->length + 1) > MAX_SPAN) return PNN_ERR_TOO_LARGE;
+  if (d->batch > MAX_COUNT || d->length > (1 << 30) || d->channels > MAX_COUNT) return PNN_ERR_TOO_LARGE;
+  // a launch has up to 1024 threads for every 64 channels of a sequence, and the states are held densely
+  if (cdiv64(d->channels, 64) * d->batch > (1 << 21) || (__int128)d->batch * d->channels * d->length > (__int128)MAX_SPAN)
+    return PNN_ERR_TOO_LARGE;
   return PNN_OK;
 }
 

@@ -58,7 +58,10 @@ int launch_embed_bwd(const pnn_embed_desc& d, const void* dout, const void* toke
                      void* ws, hipStream_t s);
 
 // ---- recurrence ----
-constexpr int SCAN_CHUNK = 16;         // steps from one kept state to the next
+constexpr int SCAN_FS = 16, SCAN_BS = 8;   // steps of a wave in a tile, forward and backward
+constexpr int SCAN_NW = 16;                // waves of a tile of a long sequence
+constexpr int SCAN_CHUNK = SCAN_NW * SCAN_BS;   // steps from one kept state to the next
+constexpr int64_t SCAN_WGS = 256;          // workgroups that fill the device (one of 16 waves a CU)
 struct ScanArgs {
   const void *x, *gate;
   const int32_t* lengths;
@@ -73,7 +76,22 @@ struct ScanArgs {
   void* ws;
 };
 inline int64_t scan_chunks(const pnn_scan_desc& d) { return cdiv64(d.length, SCAN_CHUNK); }
-inline int64_t scan_ws_bytes(const pnn_scan_desc&) { return 0; }
+// Ranges a sequence of `tiles` tiles is split into, given `work` channel groups in the whole batch
+inline int64_t scan_ranges(int64_t work, int64_t tiles) {
+  const int64_t r = work > 0 ? SCAN_WGS / work : 1;
+  return r < 1 ? 1 : r < tiles ? r : tiles < 1 ? 1 : tiles;
+}
+// first states, then (A, B) of every range; 0 when no sequence is split.  Covers both directions' tiles and both
+// widths of a channel group.
+inline int64_t scan_ws_bytes(const pnn_scan_desc& d) {
+  int64_t most = 1;
+  for (int vec = 1; vec <= 2; ++vec)
+    for (int steps = SCAN_BS; steps <= SCAN_FS; steps += SCAN_FS - SCAN_BS) {
+      const int64_t r = scan_ranges(d.batch * cdiv64(d.channels, 64 * vec), cdiv64(d.length, SCAN_NW * steps));
+      if (r > most) most = r;
+    }
+  return most == 1 ? 0 : round256(d.batch * d.channels * 4) + round256(d.batch * most * d.channels * 8);
+}
 int launch_scan_fwd(const pnn_scan_desc& d, const ScanArgs& a, hipStream_t s);
 int launch_scan_bwd(const pnn_scan_desc& d, const ScanArgs& a, hipStream_t s);
 
