@@ -1,21 +1,26 @@
 // Distillation loss of a row of logits z against a teacher's top logits, and its gradient:
 //   loss = alpha tau^2 sum_k p_k (log p_k - log q_{i_k}) + (1 - alpha) (-log s_y)
 //   dz_v = scale w (alpha tau (q_v - sum_{i_k = v} p_k) + (1 - alpha) (s_v - [v = y]))
-// with q = softmax(z / tau), s = softmax(z), p = softmax(teacher / tau).  One workgroup per row: a
-// pass with a running maximum and two running sums (of exp((z - m) / tau) and exp(z - m)), then a
-// pass that writes the gradient without the teacher's and the label's terms; the few classes that
-// have such terms are written again by the thread of their first entry, from the logits gathered
-// before anything was written.
+// with q = softmax(z / tau), s = softmax(z), p = softmax(teacher / tau).
+//
+// One workgroup per row.  The row is loaded once, into registers, as 16-byte pieces of the storage
+// type (NC a thread); its maximum, the sums of exponentials and the gradient are formed from there.
+// Rows too long for that are read twice (a running maximum and sums, then the gradient).  The
+// gradient is first written as if the row had neither entries nor a label; the classes that stand in
+// one are written again by the thread of their first entry, from logits gathered before any store.
+//
+// Rows may start anywhere: the whole pieces between the first and the last 16-byte boundary are the
+// row's body, the elements before and behind (fewer than two pieces) go to one thread each.
 #include "device_common.h"
+#include "seq_device.h"
 #include "seq_internal.h"
 
 namespace pnn {
 
 namespace {
 
-constexpr int THREADS = 256;
-constexpr int64_t MAX_GRID = 1 << 20;
-constexpr float LOG2E = 1.44269504f, LN2 = 0.693147181f;
+constexpr int64_t MAX_GRID = 1 << 20;   // rows of a launch
+constexpr float LOG2E = 1.44269504f;
 
 struct Distill {
   const void *z, *t;
@@ -23,130 +28,315 @@ struct Distill {
   const float* weight;
   float* loss;
   void* dz;
-  int64_t rows, z_stride, dz_stride, t_stride;
-  int classes, top;
+  int64_t row0, z_stride, dz_stride, t_stride;
+  int classes, top, t_bf16;
   float tau, alpha, scale;
 };
 
-__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
-// maximum that keeps NaN
-__device__ __forceinline__ float max_nan(float a, float b) { return a > b || a != a ? a : b; }
+// Which exponentials a row needs: one softmax (tau = 1, or only one of the two terms), both with
+// softmax(z)'s exponentials as squares or fourth powers of those of z / 2 or z / 4, or both apart.
+enum { ONE = 0, SQUARE = 1, FOURTH = 2, BOTH = 3 };
 
-// sums of exp2((z - m) kq) and exp2((z - m) log2 e) with their maximum m; joining two empty ones stays empty
-struct Stat {
-  float m, q, s;
-};
-__device__ __forceinline__ Stat join(const Stat& a, const Stat& b, float kq) {
-  Stat r;
-  r.m = max_nan(a.m, b.m);
-  const float da = a.m == r.m ? 0.0f : a.m - r.m, db = b.m == r.m ? 0.0f : b.m - r.m;
-  r.q = a.q * exp2_(da * kq) + b.q * exp2_(db * kq);
-  r.s = a.s * exp2_(da * LOG2E) + b.s * exp2_(db * LOG2E);
-  return r;
+__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// d = z - m: the exponentials of d / tau and of d (kq = log2(e) / tau; ONE: the only one's factor)
+template <int MODE>
+__device__ __forceinline__ void exps(float d, float kq, float& eq, float& es) {
+  eq = exp2_(d * kq);
+  if constexpr (MODE == ONE) es = eq;
+  if constexpr (MODE == SQUARE) es = eq * eq;
+  if constexpr (MODE == FOURTH) {
+    const float e2 = eq * eq;
+    es = e2 * e2;
+  }
+  if constexpr (MODE == BOTH) es = exp2_(d * LOG2E);
 }
 
-template <typename T, typename TT>
-__global__ __launch_bounds__(THREADS) void distill_kernel(Distill a) {
-  __shared__ float et[PNN_DISTILL_MAX_TOP + 1];   // an entry's teacher logit, then its p; the label is entry `top`
-  __shared__ float ez[PNN_DISTILL_MAX_TOP + 1];   // the student's logit of its class
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+  return v;
+}
+
+// A row of T as a body of whole 16-byte pieces and single elements before (`head`) and behind it
+template <typename T>
+struct Row {
+  const T* p;
+  int classes, head, pieces;
+  __device__ __forceinline__ Row(const void* base, int64_t off, int classes_) {
+    p = (const T*)base + off;
+    classes = classes_;
+    head = (int)((16 - ((uintptr_t)p & 15)) & 15) / (int)sizeof(T);
+    head = head < classes ? head : classes;
+    pieces = (classes - head) / St<T>::VE;
+  }
+  __device__ __forceinline__ int edges() const { return classes - pieces * St<T>::VE; }   // < 2 VE
+  // class of edge element i
+  __device__ __forceinline__ int edge(int i) const { return i < head ? i : i + pieces * St<T>::VE; }
+};
+
+template <typename T>
+__device__ __forceinline__ uint4 minus_inf() {
+  const uint32_t w = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
+  return make_uint4(w, w, w, w);
+}
+
+// The piece as loaded, not the floats an earlier sweep unpacked from it (which the compiler would keep, at twice the
+// registers), and nothing of later pieces before it.
+__device__ __forceinline__ uint4 again(uint4& u) {
+  asm volatile("" : "+v"(u.x), "+v"(u.y), "+v"(u.z), "+v"(u.w));
+  return u;
+}
+__device__ __forceinline__ uint4 load16(const void* base, uint32_t bytes) {
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  const u32x4 v = *at<const u32x4>(base, bytes);
+  return make_uint4(v.x, v.y, v.z, v.w);
+}
+__device__ __forceinline__ void piece_end() { __builtin_amdgcn_sched_barrier(0); }
+
+// NC > 0: the row in registers, NC pieces a thread; NC = 0: read twice
+template <typename T, int NT, int NC, int MODE>
+__global__ __launch_bounds__(NT, NC == 8 ? 8 : 1) void distill_kernel(Distill a) {
+  constexpr int VE = St<T>::VE, NWV = NT / 64;
+  __shared__ float et[PNN_DISTILL_MAX_TOP];       // an entry's teacher logit (-inf: no entry)
+  __shared__ float ez[PNN_DISTILL_MAX_TOP + 1];   // the student's logit of its class; the label is entry `top`
   __shared__ int ei[PNN_DISTILL_MAX_TOP + 1];     // its class, -1: none
-  __shared__ Stat wst[THREADS / 64];
-  __shared__ float wred[THREADS / 64];
-  __shared__ int bad;
+  __shared__ float wm[NWV], wt[NWV], wq[NWV], ws[NWV], wp[NWV], wk[NWV];
+  __shared__ int wbad[NWV];
   const int tid = threadIdx.x, wave = tid / 64, lane = tid & 63;
-  const float kq = LOG2E / a.tau;
-  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-  __syncthreads();                 // the row before has been read from LDS
-  const int64_t z0 = row * a.z_stride, d0 = row * a.dz_stride;
-  if (tid == 0) bad = 0;
-  __syncthreads();
+  const float inv_tau = 1.0f / a.tau;
+  // with a single softmax the label's alone is untempered
+  const float kq = MODE == ONE && a.top == 0 ? LOG2E : LOG2E / a.tau;
+  const int64_t row = a.row0 + blockIdx.x;
+  const Row<T> r(a.z, row * a.z_stride, a.classes);
+  const T* const body = r.p + r.head;
+  // the teacher's entries, ahead of the row: nothing of the row is waited for until they are in LDS
   const int y = a.labels != nullptr ? a.labels[row] : -1;
+  bool bad = false;
   float tm = -INFINITY;
-  for (int k = tid; k <= a.top; k += THREADS) {
+  int i0 = -1;
+  for (int k = tid; k <= a.top; k += NT) {
     const int i = k < a.top ? a.index[row * a.t_stride + k] : y;
-    const bool held = i >= 0 && i < a.classes;
-    if (i >= a.classes) bad = 1;
-    const float t = held && k < a.top ? St<TT>::ld(a.t, row * a.t_stride + k) : -INFINITY;
-    ei[k] = held ? i : -1;
-    ez[k] = held ? St<T>::ld(a.z, z0 + i) : 0.0f;
-    et[k] = t;
-    tm = max_nan(tm, t);
+    float t = -INFINITY;
+    if (k < a.top && i >= 0)
+      t = a.t_bf16 ? St<uint16_t>::ld(a.t, row * a.t_stride + k) : St<float>::ld(a.t, row * a.t_stride + k);
+    bad |= i >= a.classes;
+    i0 = i >= 0 && i < a.classes ? i : -1;
+    ei[k] = i0;
+    if (k < a.top) et[k] = t;
+    tm = t > tm || t != t ? t : tm;              // keeps NaN
   }
-  Stat st = {-INFINITY, 0.0f, 0.0f};
-  for (int v = tid; v < a.classes; v += THREADS) st = join(st, Stat{St<T>::ld(a.z, z0 + v), 1.0f, 1.0f}, kq);
-  for (int o = 32; o >= 1; o >>= 1) {
-    const Stat b = {__shfl_xor(st.m, o, 64), __shfl_xor(st.q, o, 64), __shfl_xor(st.s, o, 64)};
-    st = join(st, b, kq);
-    tm = max_nan(tm, __shfl_xor(tm, o, 64));
-  }
-  if (lane == 0) {
-    wst[wave] = st;
-    wred[wave] = tm;
-  }
-  __syncthreads();
-  st = wst[0];
-  tm = wred[0];
-  for (int w = 1; w < THREADS / 64; ++w) {
-    st = join(st, wst[w], kq);
-    tm = max_nan(tm, wred[w]);
-  }
-  const bool some = tm != -INFINITY;       // an entry with a finite (or NaN) teacher logit
-  float ts = 0.0f;
-  for (int k = tid; k < a.top; k += THREADS) ts += some ? exp2_((et[k] - tm) * kq) : 0.0f;
-  ts = wave_sum(ts);
-  __syncthreads();
-  if (lane == 0) wred[wave] = ts;
-  __syncthreads();
-  ts = 0.0f;
-  for (int w = 0; w < THREADS / 64; ++w) ts += wred[w];
-  // loss: log p_k - log q_k = (t_k - tm) / tau - log ts - (z_k - m) / tau + log sum_q
-  const float lq = logf(st.q), lt = logf(ts), inv_tau = 1.0f / a.tau;
-  float kl = 0.0f;
-  for (int k = tid; k < a.top; k += THREADS) {
-    float p = 0.0f;
-    if (some && ei[k] >= 0) {
-      p = exp2_((et[k] - tm) * kq) / ts;
-      if (p != 0.0f) kl += p * (((et[k] - tm) * inv_tau - lt) - ((ez[k] - st.m) * inv_tau - lq));
+  uint4 raw[NC > 0 ? NC : 1];
+  if constexpr (NC > 0) {
+#pragma unroll
+    for (int j = 0; j < NC; ++j) {
+      raw[j] = minus_inf<T>();
+      if (j * NT + tid < r.pieces) raw[j] = load16(body + j * NT * VE, tid * 16);
     }
-    et[k] = p;
   }
-  kl = wave_sum(kl);
+  const bool has_edge = tid < r.edges();
+  const int ve = r.edge(tid);
+  const float edge = has_edge ? St<T>::ld(r.p, ve) : -INFINITY;
+  for (int k = tid; k <= a.top; k += NT) {
+    const int i = k + NT > a.top ? i0 : ei[k];   // the last round's is still at hand
+    ez[k] = i >= 0 ? St<T>::ld(r.p, i) : 0.0f;
+  }
+  // maximum of the row; with the row read twice also the thread's sums about its own maximum
+  float m = edge, sq = 0.0f, ss = 0.0f;
+  if constexpr (NC > 0) {
+#pragma unroll
+    for (int j = 0; j < NC; ++j) {
+      Chunk<T> v;
+      unpack_chunk<T>(again(raw[j]), v);
+#pragma unroll
+      for (int e = 0; e < VE; ++e) m = fmaxf(m, v.v[e]);
+    }
+  } else {
+    if (has_edge) sq = ss = 1.0f;
+    for (int c = tid; c < r.pieces; c += NT) {
+      Chunk<T> v;
+      unpack_chunk<T>(((const uint4*)body)[c], v);
+      float cm = v.v[0];
+#pragma unroll
+      for (int e = 1; e < VE; ++e) cm = fmaxf(cm, v.v[e]);
+      if (cm > m) {
+        float eq, es;
+        exps<MODE>(m - cm, kq, eq, es);          // from m = -inf: 0
+        sq *= eq;
+        ss *= es;
+        m = cm;
+      }
+#pragma unroll
+      for (int e = 0; e < VE; ++e) {
+        float eq, es;
+        // -inf - -inf stays out while the thread has seen nothing else
+        exps<MODE>(v.v[e] == -INFINITY ? -INFINITY : v.v[e] - m, kq, eq, es);
+        sq += eq;
+        ss += es;
+      }
+    }
+  }
+  const float own = m;
+  m = wave_max(m);
+  bool nan = tm != tm;
+  tm = wave_max(tm);
+  const int flags = (__any(bad) ? 1 : 0) | (__any(nan) ? 2 : 0);
+  if (lane == 0) {
+    wm[wave] = m;
+    wt[wave] = tm;
+    wbad[wave] = flags;
+  }
   __syncthreads();
-  if (lane == 0) wred[wave] = kl;
+  int all = 0;
+#pragma unroll 4
+  for (int w = 0; w < NWV; ++w) {
+    m = fmaxf(m, wm[w]);
+    tm = fmaxf(tm, wt[w]);
+    all |= wbad[w];
+  }
+  bad = all & 1;
+  if (all & 2) tm = __builtin_nanf("");
+  const bool some = tm != -INFINITY;             // an entry with a finite (or NaN) teacher logit
+  // sums of exponentials: of the row about m, of the teacher's entries about tm
+  if constexpr (NC > 0) {
+    float eq, es;
+    exps<MODE>(edge - m, kq, eq, es);
+    if (has_edge) {
+      sq = eq;
+      ss = es;
+    }
+#pragma unroll
+    for (int j = 0; j < NC; ++j) {
+      Chunk<T> v;
+      unpack_chunk<T>(again(raw[j]), v);
+#pragma unroll
+      for (int e = 0; e < VE; ++e) {
+        exps<MODE>(v.v[e] - m, kq, eq, es);
+        sq += eq;
+        if constexpr (MODE != ONE) ss += es;
+      }
+      piece_end();
+    }
+  } else {
+    float eq, es;
+    exps<MODE>(own == -INFINITY ? -INFINITY : own - m, kq, eq, es);
+    sq *= eq;
+    ss *= es;
+    if (m == -INFINITY) sq = ss = __builtin_nanf("");   // nothing but -inf: no distribution
+  }
+  float ts = 0.0f;
+  for (int k = tid; k < a.top; k += NT) ts += some ? exp2_((et[k] - tm) * kq) : 0.0f;
+  sq = wave_sum(sq);
+  if constexpr (MODE != ONE) ss = wave_sum(ss);
+  ts = wave_sum(ts);
+  if (lane == 0) {
+    wq[wave] = sq;
+    ws[wave] = ss;
+    wp[wave] = ts;
+  }
   __syncthreads();
+  sq = ss = ts = 0.0f;
+#pragma unroll 4
+  for (int w = 0; w < NWV; ++w) {
+    sq += wq[w];
+    if constexpr (MODE != ONE) ss += ws[w];
+    ts += wp[w];
+  }
+  if constexpr (MODE == ONE) ss = sq;
+  // log p_k - log q_k = (t_k - tm) / tau - log ts - (z_k - m) / tau + log sq
+  const float inv_ts = 1.0f / ts, lqt = logf(sq) - logf(ts);
+  float kl = 0.0f;
+  for (int k = tid; k < a.top; k += NT) {
+    if (!some || ei[k] < 0) continue;
+    const float p = exp2_((et[k] - tm) * kq) * inv_ts;
+    if (p != 0.0f) kl += p * (((et[k] - tm) - (ez[k] - m)) * inv_tau + lqt);
+  }
   const bool hard = y >= 0;
-  if (tid == 0) {
-    float l = 0.0f;
-    for (int w = 0; w < THREADS / 64; ++w) l += wred[w];
-    l *= a.alpha * a.tau * a.tau;
-    if (hard) l += (1.0f - a.alpha) * (logf(st.s) - (ez[a.top] - st.m));
-    a.loss[row] = bad ? __builtin_nanf("") : l;
-  }
-  if (a.dz == nullptr) continue;
-  if (!some && !hard && !bad) {    // neither term: no gradient, whatever the logits
-    for (int v = tid; v < a.classes; v += THREADS) St<T>::st(a.dz, d0 + v, 0.0f);
-    continue;
-  }
   float g = a.scale * (a.weight != nullptr ? a.weight[row] : 1.0f);
   if (bad) g = __builtin_nanf("");
   const float gq = g * a.alpha * a.tau, gs = g * (1.0f - a.alpha);
-  const float cq = (some || bad ? gq : 0.0f) / st.q, cs = (hard ? gs : 0.0f) / st.s;
-  auto base = [&](float z) { return cq * exp2_((z - st.m) * kq) + cs * exp2_((z - st.m) * LOG2E); };
-  for (int v = tid; v < a.classes; v += THREADS) St<T>::st(a.dz, d0 + v, base(St<T>::ld(a.z, z0 + v)));
-  __syncthreads();
-  for (int k = tid; k <= a.top; k += THREADS) {
-    const int i = ei[k];
-    if (i < 0) continue;
-    bool first = true;
-    float p = 0.0f;
-    for (int j = 0; j < a.top; ++j)
-      if (ei[j] == i) {
-        if (j < k) first = false;
-        p += et[j];
+  const float cq = some || bad ? gq / sq : 0.0f, cs = hard ? gs / ss : 0.0f;
+  const bool zero = !some && !hard && !bad;      // neither term: no gradient, whatever the logits
+  auto grad = [&](float z) {
+    float eq, es;
+    exps<MODE>(z - m, kq, eq, es);
+    if constexpr (MODE == ONE) return zero ? 0.0f : (cq + cs) * eq;
+    return zero ? 0.0f : fmaf(cq, eq, cs * es);
+  };
+  if (a.dz != nullptr) {
+    T* const dp = (T*)a.dz + row * a.dz_stride;
+    const bool together = (((uintptr_t)(dp + r.head)) & 15) == 0;   // the gradient's pieces are the row's
+    auto put = [&](int c, uint4 u) {
+      Chunk<T> v;
+      unpack_chunk<T>(u, v);
+#pragma unroll
+      for (int e = 0; e < VE; ++e) v.v[e] = grad(v.v[e]);
+      if (together) {
+        store_chunk<T>(dp + r.head, (int64_t)c * VE, v.v);
+      } else {
+#pragma unroll
+        for (int e = 0; e < VE; ++e) St<T>::st(dp, r.head + (int64_t)c * VE + e, v.v[e]);
       }
-    if (first) St<T>::st(a.dz, d0 + i, base(ez[k]) - gq * p - (i == y ? gs : 0.0f));
+    };
+    if constexpr (NC > 0) {
+#pragma unroll
+      for (int j = 0; j < NC; ++j) {
+        if (j * NT + tid < r.pieces) put(j * NT + tid, again(raw[j]));
+        piece_end();
+      }
+    } else {
+      for (int c = tid; c < r.pieces; c += NT) put(c, ((const uint4*)body)[c]);
+    }
+    if (has_edge) St<T>::st(dp, ve, grad(edge));
   }
+  kl = wave_sum(kl);
+  if (lane == 0) wk[wave] = kl;
+  __syncthreads();                               // also: the stores above are before those below
+  if (tid == 0) {
+    float l = 0.0f;
+#pragma unroll
+    for (int w = 0; w < NWV; ++w) l += wk[w];
+    l *= a.alpha * a.tau * a.tau;
+    if (hard) l += (1.0f - a.alpha) * (logf(ss) - (ez[a.top] - m));
+    a.loss[row] = bad ? __builtin_nanf("") : l;
   }
+  if (a.dz != nullptr && !zero && !bad) {
+    for (int k = tid; k <= a.top; k += NT) {
+      const int i = ei[k];
+      if (i < 0) continue;
+      bool first = true;
+      float p = 0.0f;
+      for (int j = 0; j < a.top; ++j)
+        if (ei[j] == i) {
+          if (j < k) first = false;
+          if (some) p += exp2_((et[j] - tm) * kq) * inv_ts;
+        }
+      if (first) St<T>::st(a.dz, row * a.dz_stride + i, grad(ez[k]) - gq * p - (i == y ? gs : 0.0f));
+    }
+  }
+}
+
+// a row's pieces at most: the first and the last boundary may lie inside the row
+template <typename T, int MODE>
+void launch_rows(const Distill& a, int64_t rows, hipStream_t s) {
+  const dim3 grid((unsigned)rows);
+  const int pieces = a.classes / St<T>::VE;
+#define ROWS(NT, NC) hipLaunchKernelGGL((distill_kernel<T, NT, NC, MODE>), grid, dim3(NT), 0, s, a)
+  if (pieces <= 64 * 4) ROWS(64, 4);
+  else if (pieces <= 256 * 4) ROWS(256, 4);
+  else if (pieces <= 512 * 8) ROWS(512, 8);
+  else if (pieces <= 1024 * 8) ROWS(1024, 8);
+  else if (pieces <= 1024 * 16) ROWS(1024, 16);
+  else ROWS(1024, 0);
+#undef ROWS
+}
+
+template <typename T>
+void launch_mode(const Distill& a, int64_t rows, hipStream_t s) {
+  if (a.labels == nullptr || a.top == 0 || a.tau == 1.0f) launch_rows<T, ONE>(a, rows, s);
+  else if (a.tau == 2.0f) launch_rows<T, SQUARE>(a, rows, s);
+  else if (a.tau == 4.0f) launch_rows<T, FOURTH>(a, rows, s);
+  else launch_rows<T, BOTH>(a, rows, s);
 }
 
 }  // namespace
@@ -157,29 +347,26 @@ int launch_distill(const pnn_distill_desc& d, const void* logits, const int32_t*
   a.z = logits;
   a.t = teacher;
   a.index = index;
-  a.labels = labels;
+  a.labels = d.alpha == 1.0f ? nullptr : labels;   // a term of weight zero is left out
   a.weight = weight;
   a.loss = loss;
   a.dz = dlogits;
-  a.rows = d.rows;
   a.z_stride = d.logit_stride;
   a.dz_stride = d.grad_stride;
   a.t_stride = d.top_stride;
   a.classes = (int)d.classes;
-  a.top = (int)d.top;
+  a.top = d.alpha == 0.0f ? 0 : (int)d.top;
+  a.t_bf16 = d.teacher_dtype == PNN_BF16;
   a.tau = d.temperature;
   a.alpha = d.alpha;
   a.scale = d.scale;
-  const dim3 grid((unsigned)(d.rows < MAX_GRID ? d.rows : MAX_GRID)), block(THREADS);
-#define ROWS(T)                                                                                                 \
-  do {                                                                                                          \
-    if (d.teacher_dtype == PNN_F32) hipLaunchKernelGGL((distill_kernel<T, float>), grid, block, 0, s, a);       \
-    else hipLaunchKernelGGL((distill_kernel<T, uint16_t>), grid, block, 0, s, a);                               \
-  } while (0)
-  if (d.dtype == PNN_F32) ROWS(float);
-  else ROWS(uint16_t);
-#undef ROWS
-  return (int)hipGetLastError();
+  for (a.row0 = 0; a.row0 < d.rows; a.row0 += MAX_GRID) {
+    const int64_t rows = d.rows - a.row0 < MAX_GRID ? d.rows - a.row0 : MAX_GRID;
+    if (d.dtype == PNN_F32) launch_mode<float>(a, rows, s);
+    else launch_mode<uint16_t>(a, rows, s);
+    if (const hipError_t e = hipGetLastError()) return (int)e;
+  }
+  return 0;
 }
 
 }  // namespace pnn

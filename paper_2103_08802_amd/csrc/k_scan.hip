@@ -15,6 +15,7 @@
 // the ranges before (backward: behind) it, in order.  That launch reads x and gate (backward: gate
 // and dh) a second time.
 #include "device_common.h"
+#include "seq_device.h"
 #include "seq_internal.h"
 
 namespace pnn {
@@ -72,18 +73,6 @@ template <> struct Raw<float, 1> {
   __device__ static __forceinline__ U put(const float* v) { return v[0]; }
 };
 
-// Channel c of a row that is the same for all lanes: a scalar address and a 32-bit lane offset.  The empty asm pins
-// each to its kind of register here; without it the compiler holds a 64-bit address a lane for every step (the VEC 2
-// backward then spills 250 bytes).
-template <typename T, typename U, typename P>
-__device__ __forceinline__ auto at(P* row, int c) {
-  typedef typename std::conditional<std::is_const<U>::value, const char, char>::type B;
-  __attribute__((address_space(1))) B* r = (__attribute__((address_space(1))) B*)row;
-  uint32_t o = (uint32_t)c * (uint32_t)sizeof(T);
-  asm volatile("" : "+s"(r), "+v"(o));
-  return (__attribute__((address_space(1))) U*)(r + o);
-}
-
 // Steps t0 .. t0 + S - 1 of one channel group, the ones from `end` on as `none`.  t0 and end are the
 // same for all lanes.
 template <typename T, int VEC, int S>
@@ -93,10 +82,10 @@ __device__ __forceinline__ void load_steps(typename Raw<T, VEC>::U (&r)[S], cons
   const T* p = (const T*)base + (b * st.batch + (int64_t)t0 * st.step);
   if (t0 + S <= end) {
 #pragma unroll
-    for (int s = 0; s < S; ++s) r[s] = *at<T, const U>(p + s * st.step, c);
+    for (int s = 0; s < S; ++s) r[s] = *at<const U>(p + s * st.step, c * sizeof(T));
   } else {
 #pragma unroll
-    for (int s = 0; s < S; ++s) r[s] = t0 + s < end ? *at<T, const U>(p + s * st.step, c) : none;
+    for (int s = 0; s < S; ++s) r[s] = t0 + s < end ? *at<const U>(p + s * st.step, c * sizeof(T)) : none;
   }
 }
 
@@ -290,7 +279,7 @@ __global__ __launch_bounds__(64 * NW) void scan_fwd_kernel(Dims d, ScanArgs a) {
         h[e] = fmaf(f[s][e], h[e], b[s][e]);
         o[e] = t + s < len ? h[e] : 0.0f;
       }
-      if (p.on && t + s < r1) *at<T, U>(hp + (int64_t)(t + s) * d.h.step, p.c) = Raw<T, VEC>::put(o);
+      if (p.on && t + s < r1) *at<U>(hp + (int64_t)(t + s) * d.h.step, p.c * sizeof(T)) = Raw<T, VEC>::put(o);
     }
   }
   if (a.hT != nullptr && p.range == d.ranges - 1 && p.wave == 0 && p.on)
@@ -477,8 +466,8 @@ __global__ __launch_bounds__(64 * NW) void scan_bwd_kernel(Dims d, ScanArgs a) {
         c[e] = f[s][e] * G;
       }
       if (p.on && t + s < r1) {
-        *at<T, U>(xp + (int64_t)(t + s) * d.dx.step, p.c) = Raw<T, VEC>::put(ox);
-        *at<T, U>(gp + (int64_t)(t + s) * d.dgate.step, p.c) = Raw<T, VEC>::put(og);
+        *at<U>(xp + (int64_t)(t + s) * d.dx.step, p.c * sizeof(T)) = Raw<T, VEC>::put(ox);
+        *at<U>(gp + (int64_t)(t + s) * d.dgate.step, p.c * sizeof(T)) = Raw<T, VEC>::put(og);
       }
     }
   }
