@@ -20,7 +20,7 @@ namespace pnn {
 namespace {
 
 constexpr int64_t MAX_GRID = 1 << 20;   // rows of a launch
-constexpr float LOG2E = 1.44269504f;
+constexpr float LOG2E = 1.44269504f, LN2 = 0.693147181f;
 
 struct Distill {
   const void *z, *t;
@@ -39,23 +39,40 @@ enum { ONE = 0, SQUARE = 1, FOURTH = 2, BOTH = 3 };
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// d = z - m: the exponentials of d / tau and of d (kq = log2(e) / tau; ONE: the only one's factor)
+// A row's reference point: m times the factors of the exponents, rounded once.  Exponents are formed as
+// fma(z, k, -km), everywhere the same, so the rounding of km is a common factor of a row's exponentials
+// and drops out of every quotient; logarithms of the sums are taken relative to km as well.
+struct Ref {
+  float kq, mq, ms;   // log2(e) / tau (ONE: of the only softmax), kq m, log2(e) m (BOTH)
+};
+// exponentials of z / tau and z about the reference point
 template <int MODE>
-__device__ __forceinline__ void exps(float d, float kq, float& eq, float& es) {
-  eq = exp2_(d * kq);
+__device__ __forceinline__ void exps(float z, const Ref& r, float& eq, float& es) {
+  eq = exp2_(fmaf(z, r.kq, -r.mq));
   if constexpr (MODE == ONE) es = eq;
   if constexpr (MODE == SQUARE) es = eq * eq;
   if constexpr (MODE == FOURTH) {
     const float e2 = eq * eq;
     es = e2 * e2;
   }
-  if constexpr (MODE == BOTH) es = exp2_(d * LOG2E);
+  if constexpr (MODE == BOTH) es = exp2_(fmaf(z, LOG2E, -r.ms));
 }
-
-__device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-  for (int o = 32; o >= 1; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
-  return v;
+// exponents (base 2) of those two
+__device__ __forceinline__ float exponent_q(float z, const Ref& r) { return fmaf(z, r.kq, -r.mq); }
+template <int MODE>
+__device__ __forceinline__ float exponent_s(float z, const Ref& r) {
+  return MODE == BOTH ? fmaf(z, LOG2E, -r.ms) : (MODE == SQUARE ? 2.0f : MODE == FOURTH ? 4.0f : 1.0f) * fmaf(z, r.kq, -r.mq);
+}
+template <int MODE>
+__device__ __forceinline__ Ref ref_at(float m, float kq) {
+  return Ref{kq, m * kq, MODE == BOTH ? m * LOG2E : 0.0f};
+}
+// sums about one reference point as sums about another
+template <int MODE>
+__device__ __forceinline__ void move_sums(const Ref& from, const Ref& to, float& sq, float& ss) {
+  const float e = exp2_(from.mq - to.mq);
+  sq *= e;
+  ss *= MODE == BOTH ? exp2_(from.ms - to.ms) : MODE == SQUARE ? e * e : MODE == FOURTH ? e * e * (e * e) : e;
 }
 
 // A row of T as a body of whole 16-byte pieces and single elements before (`head`) and behind it
@@ -104,9 +121,8 @@ __global__ __launch_bounds__(NT, NC == 8 ? 8 : 1) void distill_kernel(Distill a)
   __shared__ float wm[NWV], wt[NWV], wq[NWV], ws[NWV], wp[NWV], wk[NWV];
   __shared__ int wbad[NWV];
   const int tid = threadIdx.x, wave = tid / 64, lane = tid & 63;
-  const float inv_tau = 1.0f / a.tau;
-  // with a single softmax the label's alone is untempered
-  const float kq = MODE == ONE && a.top == 0 ? LOG2E : LOG2E / a.tau;
+  const float inv_tau = 1.0f / a.tau, kt = LOG2E / a.tau;
+  const float kq = MODE == ONE && a.top == 0 ? LOG2E : kt;   // the label's softmax alone is untempered
   const int64_t row = a.row0 + blockIdx.x;
   const Row<T> r(a.z, row * a.z_stride, a.classes);
   const T* const body = r.p + r.head;
@@ -143,6 +159,7 @@ __global__ __launch_bounds__(NT, NC == 8 ? 8 : 1) void distill_kernel(Distill a)
   }
   // maximum of the row; with the row read twice also the thread's sums about its own maximum
   float m = edge, sq = 0.0f, ss = 0.0f;
+  Ref ref = {kq, 0.0f, 0.0f};                      // a thread that has seen nothing but -inf: sums stay 0
   if constexpr (NC > 0) {
 #pragma unroll
     for (int j = 0; j < NC; ++j) {
@@ -152,7 +169,10 @@ __global__ __launch_bounds__(NT, NC == 8 ? 8 : 1) void distill_kernel(Distill a)
       for (int e = 0; e < VE; ++e) m = fmaxf(m, v.v[e]);
     }
   } else {
-    if (has_edge) sq = ss = 1.0f;
+    if (m != -INFINITY) {
+      ref = ref_at<MODE>(m, kq);
+      exps<MODE>(m, ref, sq, ss);
+    }
     for (int c = tid; c < r.pieces; c += NT) {
       Chunk<T> v;
       unpack_chunk<T>(((const uint4*)body)[c], v);
@@ -160,17 +180,15 @@ __global__ __launch_bounds__(NT, NC == 8 ? 8 : 1) void distill_kernel(Distill a)
 #pragma unroll
       for (int e = 1; e < VE; ++e) cm = fmaxf(cm, v.v[e]);
       if (cm > m) {
-        float eq, es;
-        exps<MODE>(m - cm, kq, eq, es);          // from m = -inf: 0
-        sq *= eq;
-        ss *= es;
+        const Ref next = ref_at<MODE>(cm, kq);
+        if (m != -INFINITY) move_sums<MODE>(ref, next, sq, ss);
+        ref = next;
         m = cm;
       }
 #pragma unroll
       for (int e = 0; e < VE; ++e) {
         float eq, es;
-        // -inf - -inf stays out while the thread has seen nothing else
-        exps<MODE>(v.v[e] == -INFINITY ? -INFINITY : v.v[e] - m, kq, eq, es);
+        exps<MODE>(v.v[e], ref, eq, es);
         sq += eq;
         ss += es;
       }
@@ -197,10 +215,12 @@ __global__ __launch_bounds__(NT, NC == 8 ? 8 : 1) void distill_kernel(Distill a)
   bad = all & 1;
   if (all & 2) tm = __builtin_nanf("");
   const bool some = tm != -INFINITY;             // an entry with a finite (or NaN) teacher logit
+  const Ref own_ref = ref;
+  ref = ref_at<MODE>(m, kq);
   // sums of exponentials: of the row about m, of the teacher's entries about tm
   if constexpr (NC > 0) {
     float eq, es;
-    exps<MODE>(edge - m, kq, eq, es);
+    exps<MODE>(edge, ref, eq, es);
     if (has_edge) {
       sq = eq;
       ss = es;
@@ -211,24 +231,21 @@ __global__ __launch_bounds__(NT, NC == 8 ? 8 : 1) void distill_kernel(Distill a)
       unpack_chunk<T>(again(raw[j]), v);
 #pragma unroll
       for (int e = 0; e < VE; ++e) {
-        exps<MODE>(v.v[e] - m, kq, eq, es);
+        exps<MODE>(v.v[e], ref, eq, es);
         sq += eq;
         if constexpr (MODE != ONE) ss += es;
       }
       piece_end();
     }
   } else {
-    float eq, es;
-    exps<MODE>(own == -INFINITY ? -INFINITY : own - m, kq, eq, es);
-    sq *= eq;
-    ss *= es;
+    if (own != -INFINITY) move_sums<MODE>(own_ref, ref, sq, ss);
     if (m == -INFINITY) sq = ss = __builtin_nanf("");   // nothing but -inf: no distribution
   }
   float ts = 0.0f;
-  for (int k = tid; k < a.top; k += NT) ts += some ? exp2_((et[k] - tm) * kq) : 0.0f;
-  sq = wave_sum(sq);
-  if constexpr (MODE != ONE) ss = wave_sum(ss);
-  ts = wave_sum(ts);
+  for (int k = tid; k < a.top; k += NT) ts += some ? exp2_((et[k] - tm) * kt) : 0.0f;
+  sq = wave_add(sq);
+  if constexpr (MODE != ONE) ss = wave_add(ss);
+  ts = wave_add(ts);
   if (lane == 0) {
     wq[wave] = sq;
     ws[wave] = ss;
@@ -243,13 +260,13 @@ __global__ __launch_bounds__(NT, NC == 8 ? 8 : 1) void distill_kernel(Distill a)
     ts += wp[w];
   }
   if constexpr (MODE == ONE) ss = sq;
-  // log p_k - log q_k = (t_k - tm) / tau - log ts - (z_k - m) / tau + log sq
+  // log p_k - log q_k = (t_k - tm) / tau - log ts - ln2 (exponent of z_k) + log sq
   const float inv_ts = 1.0f / ts, lqt = logf(sq) - logf(ts);
   float kl = 0.0f;
   for (int k = tid; k < a.top; k += NT) {
     if (!some || ei[k] < 0) continue;
-    const float p = exp2_((et[k] - tm) * kq) * inv_ts;
-    if (p != 0.0f) kl += p * (((et[k] - tm) - (ez[k] - m)) * inv_tau + lqt);
+    const float p = exp2_((et[k] - tm) * kt) * inv_ts;
+    if (p != 0.0f) kl += p * (fmaf(et[k] - tm, inv_tau, -LN2 * exponent_q(ez[k], ref)) + lqt);
   }
   const bool hard = y >= 0;
   float g = a.scale * (a.weight != nullptr ? a.weight[row] : 1.0f);
@@ -259,7 +276,7 @@ __global__ __launch_bounds__(NT, NC == 8 ? 8 : 1) void distill_kernel(Distill a)
   const bool zero = !some && !hard && !bad;      // neither term: no gradient, whatever the logits
   auto grad = [&](float z) {
     float eq, es;
-    exps<MODE>(z - m, kq, eq, es);
+    exps<MODE>(z, ref, eq, es);
     if constexpr (MODE == ONE) return zero ? 0.0f : (cq + cs) * eq;
     return zero ? 0.0f : fmaf(cq, eq, cs * es);
   };
@@ -289,7 +306,7 @@ __global__ __launch_bounds__(NT, NC == 8 ? 8 : 1) void distill_kernel(Distill a)
     }
     if (has_edge) St<T>::st(dp, ve, grad(edge));
   }
-  kl = wave_sum(kl);
+  kl = wave_add(kl);
   if (lane == 0) wk[wave] = kl;
   __syncthreads();                               // also: the stores above are before those below
   if (tid == 0) {
@@ -297,7 +314,7 @@ __global__ __launch_bounds__(NT, NC == 8 ? 8 : 1) void distill_kernel(Distill a)
 #pragma unroll
     for (int w = 0; w < NWV; ++w) l += wk[w];
     l *= a.alpha * a.tau * a.tau;
-    if (hard) l += (1.0f - a.alpha) * (logf(ss) - (ez[a.top] - m));
+    if (hard) l += (1.0f - a.alpha) * (logf(ss) - LN2 * exponent_s<MODE>(ez[a.top], ref));
     a.loss[row] = bad ? __builtin_nanf("") : l;
   }
   if (a.dz != nullptr && !zero && !bad) {
@@ -309,7 +326,7 @@ __global__ __launch_bounds__(NT, NC == 8 ? 8 : 1) void distill_kernel(Distill a)
       for (int j = 0; j < a.top; ++j)
         if (ei[j] == i) {
           if (j < k) first = false;
-          if (some) p += exp2_((et[j] - tm) * kq) * inv_ts;
+          if (some) p += exp2_((et[j] - tm) * kt) * inv_ts;
         }
       if (first) St<T>::st(a.dz, row * a.dz_stride + i, grad(ez[k]) - gq * p - (i == y ? gs : 0.0f));
     }

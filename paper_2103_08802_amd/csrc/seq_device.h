@@ -19,4 +19,26 @@ __device__ __forceinline__ auto at(P* base, uint32_t bytes) {
   return (__attribute__((address_space(1))) U*)(r + bytes);
 }
 
+// The wave's sum / maximum in every lane, in a fixed order, without LDS: DPP exchanges within rows of 16 lanes, then
+// the four rows by scalar reads.
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
+template <typename F>
+__device__ __forceinline__ float wave_fold(float v, F f) {
+  v = f(v, dpp<0xB1>(v));    // quad_perm 1 0 3 2
+  v = f(v, dpp<0x4E>(v));    // quad_perm 2 3 0 1
+  v = f(v, dpp<0x141>(v));   // row_half_mirror
+  v = f(v, dpp<0x140>(v));   // row_mirror
+  auto row = [&](int l) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), l)); };
+  return f(f(row(0), row(16)), f(row(32), row(48)));
+}
+__device__ __forceinline__ float wave_add(float v) {
+  return wave_fold(v, [](float a, float b) { return a + b; });
+}
+__device__ __forceinline__ float wave_max(float v) {
+  return wave_fold(v, [](float a, float b) { return fmaxf(a, b); });
+}
+
 }  // namespace pnn
