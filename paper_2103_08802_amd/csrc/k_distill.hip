@@ -57,6 +57,20 @@ __device__ __forceinline__ void exps(float z, const Ref& r, float& eq, float& es
   }
   if constexpr (MODE == BOTH) es = exp2_(fmaf(z, LOG2E, -r.ms));
 }
+// four elements' exponentials added to the sums; the four exponentials stand together, ahead of their uses
+template <int MODE>
+__device__ __forceinline__ void add_exps(const float* z, const Ref& r, float& sq, float& ss) {
+  float eq[4], es[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) exps<MODE == BOTH ? BOTH : ONE>(z[e], r, eq[e], es[e]);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    sq += eq[e];
+    if constexpr (MODE == SQUARE) ss = fmaf(eq[e], eq[e], ss);
+    if constexpr (MODE == FOURTH) ss = fmaf(eq[e] * eq[e], eq[e] * eq[e], ss);
+    if constexpr (MODE == BOTH) ss += es[e];
+  }
+}
 // exponents (base 2) of those two
 __device__ __forceinline__ float exponent_q(float z, const Ref& r) { return fmaf(z, r.kq, -r.mq); }
 template <int MODE>
@@ -186,12 +200,7 @@ __global__ __launch_bounds__(NT, NC == 8 ? 8 : 1) void distill_kernel(Distill a)
         m = cm;
       }
 #pragma unroll
-      for (int e = 0; e < VE; ++e) {
-        float eq, es;
-        exps<MODE>(v.v[e], ref, eq, es);
-        sq += eq;
-        ss += es;
-      }
+      for (int e = 0; e < VE; e += 4) add_exps<MODE>(v.v + e, ref, sq, ss);
     }
   }
   const float own = m;
@@ -230,11 +239,7 @@ __global__ __launch_bounds__(NT, NC == 8 ? 8 : 1) void distill_kernel(Distill a)
       Chunk<T> v;
       unpack_chunk<T>(again(raw[j]), v);
 #pragma unroll
-      for (int e = 0; e < VE; ++e) {
-        exps<MODE>(v.v[e], ref, eq, es);
-        sq += eq;
-        if constexpr (MODE != ONE) ss += es;
-      }
+      for (int e = 0; e < VE; e += 4) add_exps<MODE>(v.v + e, ref, sq, ss);
       piece_end();
     }
   } else {
@@ -274,11 +279,14 @@ __global__ __launch_bounds__(NT, NC == 8 ? 8 : 1) void distill_kernel(Distill a)
   const float gq = g * a.alpha * a.tau, gs = g * (1.0f - a.alpha);
   const float cq = some || bad ? gq / sq : 0.0f, cs = hard ? gs / ss : 0.0f;
   const bool zero = !some && !hard && !bad;      // neither term: no gradient, whatever the logits
-  auto grad = [&](float z) {
+  const float c1 = cq + cs;
+  auto grad = [&](float z) {                     // cq eq + cs es
     float eq, es;
-    exps<MODE>(z, ref, eq, es);
-    if constexpr (MODE == ONE) return zero ? 0.0f : (cq + cs) * eq;
-    return zero ? 0.0f : fmaf(cq, eq, cs * es);
+    exps<MODE == BOTH ? BOTH : ONE>(z, ref, eq, es);
+    if constexpr (MODE == ONE) return c1 * eq;
+    if constexpr (MODE == SQUARE) return fmaf(cs, eq, cq) * eq;
+    if constexpr (MODE == FOURTH) return fmaf(cs, eq * eq * eq, cq) * eq;
+    return fmaf(cq, eq, cs * es);
   };
   if (a.dz != nullptr) {
     T* const dp = (T*)a.dz + row * a.dz_stride;
@@ -289,13 +297,15 @@ __global__ __launch_bounds__(NT, NC == 8 ? 8 : 1) void distill_kernel(Distill a)
 #pragma unroll
       for (int e = 0; e < VE; ++e) v.v[e] = grad(v.v[e]);
       if (together) {
-        store_chunk<T>(dp + r.head, (int64_t)c * VE, v.v);
+        store_pairs<T>(dp + r.head, (int64_t)c * VE, v.v);
       } else {
 #pragma unroll
         for (int e = 0; e < VE; ++e) St<T>::st(dp, r.head + (int64_t)c * VE + e, v.v[e]);
       }
     };
-    if constexpr (NC > 0) {
+    if (zero) {
+      for (int v = tid; v < a.classes; v += NT) St<T>::st(dp, v, 0.0f);
+    } else if constexpr (NC > 0) {
 #pragma unroll
       for (int j = 0; j < NC; ++j) {
         if (j * NT + tid < r.pieces) put(j * NT + tid, again(raw[j]));
@@ -304,7 +314,7 @@ __global__ __launch_bounds__(NT, NC == 8 ? 8 : 1) void distill_kernel(Distill a)
     } else {
       for (int c = tid; c < r.pieces; c += NT) put(c, ((const uint4*)body)[c]);
     }
-    if (has_edge) St<T>::st(dp, ve, grad(edge));
+    if (has_edge && !zero) St<T>::st(dp, ve, grad(edge));
   }
   kl = wave_add(kl);
   if (lane == 0) wk[wave] = kl;

@@ -19,6 +19,19 @@ __device__ __forceinline__ auto at(P* base, uint32_t bytes) {
   return (__attribute__((address_space(1))) U*)(r + bytes);
 }
 
+// One 16-byte piece of T at element i, two bf16 to a conversion.
+template <typename T>
+__device__ __forceinline__ void store_pairs(void* base, int64_t i, const float* v) {
+  if constexpr (sizeof(T) == 4) {
+    *(float4*)((float*)base + i) = make_float4(v[0], v[1], v[2], v[3]);
+  } else {
+    typedef float f32x8 __attribute__((ext_vector_type(8)));
+    typedef __bf16 bf16x8_ __attribute__((ext_vector_type(8)));
+    const f32x8 f = {v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]};
+    *(bf16x8_*)((uint16_t*)base + i) = __builtin_convertvector(f, bf16x8_);
+  }
+}
+
 // The wave's sum / maximum in every lane, in a fixed order, without LDS: DPP exchanges within rows of 16 lanes, then
 // the four rows by scalar reads.
 template <int CTRL>
