@@ -29,7 +29,7 @@ struct Distill {
   float* loss;
   void* dz;
   int64_t row0, z_stride, dz_stride, t_stride;
-  int classes, top, t_bf16;
+  int classes, top, t_bf16, past;
   float tau, alpha, scale;
 };
 
@@ -129,9 +129,10 @@ __device__ __forceinline__ void piece_end() { __builtin_amdgcn_sched_barrier(0);
 template <typename T, int NT, int NC, int MODE>
 __global__ __launch_bounds__(NT, NC == 8 ? 8 : 1) void distill_kernel(Distill a) {
   constexpr int VE = St<T>::VE, NWV = NT / 64;
-  __shared__ float et[PNN_DISTILL_MAX_TOP];       // an entry's teacher logit (-inf: no entry)
-  __shared__ float ez[PNN_DISTILL_MAX_TOP + 1];   // the student's logit of its class; the label is entry `top`
-  __shared__ int ei[PNN_DISTILL_MAX_TOP + 1];     // its class, -1: none
+  extern __shared__ float entries[];              // as many as the call has: short rows share a CU's LDS by dozens
+  float* const et = entries;                      // [top] an entry's teacher logit (-inf: no entry)
+  float* const ez = et + a.top;                   // [top + 1] the student's logit of its class; the label is entry `top`
+  int* const ei = (int*)(ez + a.top + 1);         // [top + 1] its class, -1: none
   __shared__ float wm[NWV], wt[NWV], wq[NWV], ws[NWV], wp[NWV], wk[NWV];
   __shared__ int wbad[NWV];
   const int tid = threadIdx.x, wave = tid / 64, lane = tid & 63;
@@ -297,7 +298,7 @@ __global__ __launch_bounds__(NT, NC == 8 ? 8 : 1) void distill_kernel(Distill a)
 #pragma unroll
       for (int e = 0; e < VE; ++e) v.v[e] = grad(v.v[e]);
       if (together) {
-        store_pairs<T>(dp + r.head, (int64_t)c * VE, v.v);
+        store_piece<T>(dp + r.head, (int64_t)c * VE, v.v, a.past);
       } else {
 #pragma unroll
         for (int e = 0; e < VE; ++e) St<T>::st(dp, r.head + (int64_t)c * VE + e, v.v[e]);
@@ -348,7 +349,7 @@ template <typename T, int MODE>
 void launch_rows(const Distill& a, int64_t rows, hipStream_t s) {
   const dim3 grid((unsigned)rows);
   const int pieces = a.classes / St<T>::VE;
-#define ROWS(NT, NC) hipLaunchKernelGGL((distill_kernel<T, NT, NC, MODE>), grid, dim3(NT), 0, s, a)
+#define ROWS(NT, NC) hipLaunchKernelGGL((distill_kernel<T, NT, NC, MODE>), grid, dim3(NT), (3 * a.top + 2) * 4, s, a)
   if (pieces <= 64 * 4) ROWS(64, 4);
   else if (pieces <= 256 * 4) ROWS(256, 4);
   else if (pieces <= 512 * 8) ROWS(512, 8);
@@ -384,6 +385,7 @@ int launch_distill(const pnn_distill_desc& d, const void* logits, const int32_t*
   a.classes = (int)d.classes;
   a.top = d.alpha == 0.0f ? 0 : (int)d.top;
   a.t_bf16 = d.teacher_dtype == PNN_BF16;
+  a.past = d.rows * d.classes * (d.dtype == PNN_F32 ? 4 : 2) > L2_BYTES;
   a.tau = d.temperature;
   a.alpha = d.alpha;
   a.scale = d.scale;
