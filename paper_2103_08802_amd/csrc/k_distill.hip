@@ -30,6 +30,7 @@ struct Distill {
   void* dz;
   int64_t row0, z_stride, dz_stride, t_stride;
   int classes, top, t_bf16, past;
+  int hash_mask;                 // a power of two above 2 top, less one
   float tau, alpha, scale;
 };
 
@@ -133,6 +134,8 @@ __global__ __launch_bounds__(NT, NC == 8 ? 8 : 1) void distill_kernel(Distill a)
   float* const et = entries;                      // [top] an entry's teacher logit (-inf: no entry)
   float* const ez = et + a.top;                   // [top + 1] the student's logit of its class; the label is entry `top`
   int* const ei = (int*)(ez + a.top + 1);         // [top + 1] its class, -1: none
+  int* const table = ei + a.top + 1;              // [hash_mask + 1] classes of entries, hashed
+  __shared__ int twice, listed;
   __shared__ float wm[NWV], wt[NWV], wq[NWV], ws[NWV], wp[NWV], wk[NWV];
   __shared__ int wbad[NWV];
   const int tid = threadIdx.x, wave = tid / 64, lane = tid & 63;
@@ -141,21 +144,18 @@ __global__ __launch_bounds__(NT, NC == 8 ? 8 : 1) void distill_kernel(Distill a)
   const int64_t row = a.row0 + blockIdx.x;
   const Row<T> r(a.z, row * a.z_stride, a.classes);
   const T* const body = r.p + r.head;
-  // the teacher's entries, ahead of the row: nothing of the row is waited for until they are in LDS
+  // loads: the thread's first teacher entry, the row, then (what depends on it) the entry's class
   const int y = a.labels != nullptr ? a.labels[row] : -1;
-  bool bad = false;
-  float tm = -INFINITY;
+  auto teacher = [&](int k) {
+    return a.t_bf16 ? St<uint16_t>::ld(a.t, row * a.t_stride + k) : St<float>::ld(a.t, row * a.t_stride + k);
+  };
   int i0 = -1;
-  for (int k = tid; k <= a.top; k += NT) {
-    const int i = k < a.top ? a.index[row * a.t_stride + k] : y;
-    float t = -INFINITY;
-    if (k < a.top && i >= 0)
-      t = a.t_bf16 ? St<uint16_t>::ld(a.t, row * a.t_stride + k) : St<float>::ld(a.t, row * a.t_stride + k);
-    bad |= i >= a.classes;
-    i0 = i >= 0 && i < a.classes ? i : -1;
-    ei[k] = i0;
-    if (k < a.top) et[k] = t;
-    tm = t > tm || t != t ? t : tm;              // keeps NaN
+  float t0 = 0.0f, z0 = 0.0f;
+  if (tid < a.top) {
+    i0 = a.index[row * a.t_stride + tid];
+    t0 = teacher(tid);
+  } else if (tid == a.top) {
+    i0 = y;
   }
   uint4 raw[NC > 0 ? NC : 1];
   if constexpr (NC > 0) {
@@ -168,9 +168,26 @@ __global__ __launch_bounds__(NT, NC == 8 ? 8 : 1) void distill_kernel(Distill a)
   const bool has_edge = tid < r.edges();
   const int ve = r.edge(tid);
   const float edge = has_edge ? St<T>::ld(r.p, ve) : -INFINITY;
-  for (int k = tid; k <= a.top; k += NT) {
-    const int i = k + NT > a.top ? i0 : ei[k];   // the last round's is still at hand
-    ez[k] = i >= 0 ? St<T>::ld(r.p, i) : 0.0f;
+  for (int h = tid; h <= a.hash_mask; h += NT) table[h] = -1;
+  if (tid == 0) twice = listed = 0;
+  bool bad = false;
+  float tm = -INFINITY;
+  auto entry = [&](int k, int& i, float t) {       // entry k's class (-1: none) and teacher logit to LDS
+    bad |= i >= a.classes;
+    if (k < a.top) {
+      t = i >= 0 ? t : -INFINITY;
+      et[k] = t;
+      tm = t > tm || t != t ? t : tm;              // keeps NaN
+    }
+    i = i >= 0 && i < a.classes ? i : -1;
+    ei[k] = i;
+    return i >= 0 ? St<T>::ld(r.p, i) : 0.0f;
+  };
+  if (tid <= a.top) z0 = entry(tid, i0, t0);       // to LDS only when the row has been summed
+  for (int k = tid + NT; k <= a.top; k += NT) {
+    int i = k < a.top ? a.index[row * a.t_stride + k] : y;
+    const float t = k < a.top ? teacher(k) : 0.0f;
+    ez[k] = entry(k, i, t);
   }
   // maximum of the row; with the row read twice also the thread's sums about its own maximum
   float m = edge, sq = 0.0f, ss = 0.0f;
@@ -247,8 +264,21 @@ __global__ __launch_bounds__(NT, NC == 8 ? 8 : 1) void distill_kernel(Distill a)
     if (own != -INFINITY) move_sums<MODE>(own_ref, ref, sq, ss);
     if (m == -INFINITY) sq = ss = __builtin_nanf("");   // nothing but -inf: no distribution
   }
+  // the teacher's sum; whether a class stands in two entries, and whether the label's stands in one
   float ts = 0.0f;
-  for (int k = tid; k < a.top; k += NT) ts += some ? exp2_((et[k] - tm) * kt) : 0.0f;
+  for (int k = tid; k < a.top; k += NT) {
+    ts += some ? exp2_((et[k] - tm) * kt) : 0.0f;
+    const int i = ei[k];
+    if (i < 0) continue;
+    if (i == y) listed = 1;
+    // open addressing, at most half full: every probe sequence meets the class or a free place
+    for (unsigned h = (unsigned)i * 2654435761u >> 16;; ++h) {
+      const int old = atomicCAS(&table[h & a.hash_mask], -1, i);
+      if (old == i) twice = 1;
+      if (old == i || old == -1) break;
+    }
+  }
+  if (tid <= a.top) ez[tid] = z0;
   sq = wave_add(sq);
   if constexpr (MODE != ONE) ss = wave_add(ss);
   ts = wave_add(ts);
@@ -319,7 +349,7 @@ __global__ __launch_bounds__(NT, NC == 8 ? 8 : 1) void distill_kernel(Distill a)
   }
   kl = wave_add(kl);
   if (lane == 0) wk[wave] = kl;
-  __syncthreads();                               // also: the stores above are before those below
+  __syncthreads();                               // also orders the stores above before those below (one compute unit's)
   if (tid == 0) {
     float l = 0.0f;
 #pragma unroll
@@ -332,13 +362,17 @@ __global__ __launch_bounds__(NT, NC == 8 ? 8 : 1) void distill_kernel(Distill a)
     for (int k = tid; k <= a.top; k += NT) {
       const int i = ei[k];
       if (i < 0) continue;
-      bool first = true;
+      bool first = k < a.top || !listed;
       float p = 0.0f;
-      for (int j = 0; j < a.top; ++j)
-        if (ei[j] == i) {
-          if (j < k) first = false;
-          if (some) p += exp2_((et[j] - tm) * kt) * inv_ts;
-        }
+      if (!twice) {
+        if (some && k < a.top) p = exp2_((et[k] - tm) * kt) * inv_ts;
+      } else {                                     // the first of a class's entries takes the others' p as well
+        for (int j = 0; j < a.top; ++j)
+          if (ei[j] == i) {
+            if (j < k) first = false;
+            if (some) p += exp2_((et[j] - tm) * kt) * inv_ts;
+          }
+      }
       if (first) St<T>::st(a.dz, row * a.dz_stride + i, grad(ez[k]) - gq * p - (i == y ? gs : 0.0f));
     }
   }
@@ -349,7 +383,7 @@ template <typename T, int MODE>
 void launch_rows(const Distill& a, int64_t rows, hipStream_t s) {
   const dim3 grid((unsigned)rows);
   const int pieces = a.classes / St<T>::VE;
-#define ROWS(NT, NC) hipLaunchKernelGGL((distill_kernel<T, NT, NC, MODE>), grid, dim3(NT), (3 * a.top + 2) * 4, s, a)
+#define ROWS(NT, NC) hipLaunchKernelGGL((distill_kernel<T, NT, NC, MODE>), grid, dim3(NT), (3 * a.top + 3 + a.hash_mask) * 4, s, a)
   if (pieces <= 64 * 4) ROWS(64, 4);
   else if (pieces <= 256 * 4) ROWS(256, 4);
   else if (pieces <= 512 * 8) ROWS(512, 8);
@@ -384,6 +418,8 @@ int launch_distill(const pnn_distill_desc& d, const void* logits, const int32_t*
   a.t_stride = d.top_stride;
   a.classes = (int)d.classes;
   a.top = d.alpha == 0.0f ? 0 : (int)d.top;
+  a.hash_mask = 1;
+  while (a.hash_mask < 2 * a.top) a.hash_mask = 2 * a.hash_mask + 1;
   a.t_bf16 = d.teacher_dtype == PNN_BF16;
   a.past = d.rows * d.classes * (d.dtype == PNN_F32 ? 4 : 2) > L2_BYTES;
   a.tau = d.temperature;
