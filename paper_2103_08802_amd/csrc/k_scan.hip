@@ -26,6 +26,7 @@ constexpr int FS = SCAN_FS, BS = SCAN_BS;
 
 struct Dims {
   int length, channels, groups, chunks;
+  int past;                 // results larger than the L2 caches (store_to)
   int ranges, range_tiles;  // ranges of the sequence and their tiles
   pnn_seq_stride x, gate, h, dh, dx, dgate;
   float *first;             // [batch][channels]: the state before the first (backward: gradient after the last) step
@@ -279,7 +280,7 @@ __global__ __launch_bounds__(64 * NW) void scan_fwd_kernel(Dims d, ScanArgs a) {
         h[e] = fmaf(f[s][e], h[e], b[s][e]);
         o[e] = t + s < len ? h[e] : 0.0f;
       }
-      if (p.on && t + s < r1) *at<U>(hp + (int64_t)(t + s) * d.h.step, p.c * sizeof(T)) = Raw<T, VEC>::put(o);
+      if (p.on && t + s < r1) store_to(at<U>(hp + (int64_t)(t + s) * d.h.step, p.c * sizeof(T)), Raw<T, VEC>::put(o), d.past);
     }
   }
   if (a.hT != nullptr && p.range == d.ranges - 1 && p.wave == 0 && p.on)
@@ -466,8 +467,8 @@ __global__ __launch_bounds__(64 * NW) void scan_bwd_kernel(Dims d, ScanArgs a) {
         c[e] = f[s][e] * G;
       }
       if (p.on && t + s < r1) {
-        *at<U>(xp + (int64_t)(t + s) * d.dx.step, p.c * sizeof(T)) = Raw<T, VEC>::put(ox);
-        *at<U>(gp + (int64_t)(t + s) * d.dgate.step, p.c * sizeof(T)) = Raw<T, VEC>::put(og);
+        store_to(at<U>(xp + (int64_t)(t + s) * d.dx.step, p.c * sizeof(T)), Raw<T, VEC>::put(ox), d.past);
+        store_to(at<U>(gp + (int64_t)(t + s) * d.dgate.step, p.c * sizeof(T)), Raw<T, VEC>::put(og), d.past);
       }
     }
   }
@@ -491,6 +492,7 @@ Dims dims(const pnn_scan_desc& d, const ScanArgs& a, int vec, int tile) {
   if (m.range_tiles < 1) m.range_tiles = 1;
   m.ranges = (int)cdiv64(tiles, m.range_tiles);
   if (m.ranges < 1) m.ranges = 1;
+  m.past = d.batch * d.length * d.channels * (d.dtype == PNN_F32 ? 4 : 2) > L2_BYTES;
   m.x = d.x;
   m.gate = d.gate;
   m.h = d.h;
