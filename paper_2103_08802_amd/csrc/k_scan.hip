@@ -33,24 +33,31 @@ struct Dims {
   float2 *sum;              // [batch][ranges][channels]: (A, B) of a range
 };
 
-// exp(x) for x <= 0 to about an ulp: x log2(e) in two floats, the low part to first order.
-__device__ __forceinline__ float exp_neg(float x) {
-  x = x < -120.0f ? -120.0f : x;           // exp(-120) rounds to 0 below; keeps NaN
-  const float t = x * 1.44269502f;
-  const float lo = fmaf(x, 1.44269502f, -t) + x * 1.92596299e-8f;
-  const float r = __builtin_amdgcn_exp2f(t);
-  return fmaf(r, lo * 0.693147181f, r);
-}
-
-// f = sigmoid(g) and keep = 1 - f, each to about an ulp: the smaller one is not formed by subtraction
+// f = sigmoid(g) and keep = 1 - f = exp(-g) f, each to about an ulp (keep is not formed by subtraction).
+// g is held between -87 and 100, where both are constant to the last bit and exp(-g) is finite, by
+// minimum and maximum that keep NaN.  exp(-g) = 2^t (1 + d): t = -g log2(e) rounded, d the rest of that
+// product to first order.  A bf16 g has 8 bits, so its product with the leading 16 bits of log2(e) is
+// exact; for float the rounding is recovered by a fused multiply-add, and the reciprocal is refined.
+template <typename T>
 __device__ __forceinline__ void gate_of(float g, float& f, float& keep) {
-  const float e = exp_neg(-fabsf(g));
-  const float d = 1.0f + e;
-  float r = __builtin_amdgcn_rcpf(d);
-  r = fmaf(fmaf(-d, r, 1.0f), r, r);
-  const float s = e * r;
-  f = g >= 0.0f ? r : s;
-  keep = g >= 0.0f ? s : r;
+  g = __builtin_elementwise_minimum(__builtin_elementwise_maximum(g, -87.0f), 100.0f);
+  float e, r;
+  if constexpr (sizeof(T) == 2) {
+    constexpr float HI = 1.44268798828125f;                    // 16 bits of log2(e)
+    constexpr float REST = (float)((1.4426950408889634074 - 1.44268798828125) * 0.69314718055994530942);
+    e = __builtin_amdgcn_exp2f(g * -HI) * fmaf(g, -REST, 1.0f);
+    r = __builtin_amdgcn_rcpf(1.0f + e);
+  } else {
+    constexpr float L = 1.44269502f, LO = 1.92596299e-8f;      // log2(e) in two floats
+    const float t = g * -L;
+    const float rest = fmaf(g, -LO, fmaf(g, -L, -t));
+    e = __builtin_amdgcn_exp2f(t) * fmaf(rest, 0.693147181f, 1.0f);
+    const float d = 1.0f + e;
+    r = __builtin_amdgcn_rcpf(d);
+    r = fmaf(fmaf(-d, r, 1.0f), r, r);
+  }
+  f = r;
+  keep = e * r;
 }
 
 // VEC neighbouring channels of T as they are in memory
@@ -66,7 +73,11 @@ template <> struct Raw<uint16_t, 2> {
     v[0] = __uint_as_float(u << 16);
     v[1] = __uint_as_float(u & 0xffff0000u);
   }
-  __device__ static __forceinline__ U put(const float* v) { return (uint32_t)f2bf(v[0]) | ((uint32_t)f2bf(v[1]) << 16); }
+  __device__ static __forceinline__ U put(const float* v) {
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(U, __builtin_convertvector((f32x2{v[0], v[1]}), bf16x2));
+  }
 };
 template <> struct Raw<float, 1> {
   typedef float U;
@@ -129,7 +140,7 @@ __device__ __forceinline__ void gates(const typename Raw<T, VEC>::U (&rx)[S], co
 #pragma unroll
     for (int e = 0; e < VEC; ++e) {
       float keep;
-      gate_of(g[e], f[s][e], keep);
+      gate_of<T>(g[e], f[s][e], keep);
       b[s][e] = keep * x[e];
     }
   }
@@ -179,7 +190,7 @@ __global__ __launch_bounds__(64 * NW) void scan_fwd_sum_kernel(Dims d, ScanArgs 
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
           float f, keep;
-          gate_of(g[e], f, keep);
+          gate_of<T>(g[e], f, keep);
           A[e] *= f;
           B[e] = fmaf(f, B[e], keep * x[e]);
         }
@@ -272,15 +283,24 @@ __global__ __launch_bounds__(64 * NW) void scan_fwd_kernel(Dims d, ScanArgs a) {
     if (a.states != nullptr && t % SCAN_CHUNK == 0 && t < d.length && p.on)
 #pragma unroll
       for (int e = 0; e < VEC; ++e) a.states[(p.b * d.chunks + t / SCAN_CHUNK) * d.channels + p.c + e] = h[e];
+    if (t + FS <= len) {
 #pragma unroll
-    for (int s = 0; s < FS; ++s) {
-      float o[VEC];
+      for (int s = 0; s < FS; ++s) {
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        h[e] = fmaf(f[s][e], h[e], b[s][e]);
-        o[e] = t + s < len ? h[e] : 0.0f;
+        for (int e = 0; e < VEC; ++e) h[e] = fmaf(f[s][e], h[e], b[s][e]);
+        if (p.on) store_to(at<U>(hp + (int64_t)(t + s) * d.h.step, p.c * sizeof(T)), Raw<T, VEC>::put(h), d.past);
       }
-      if (p.on && t + s < r1) store_to(at<U>(hp + (int64_t)(t + s) * d.h.step, p.c * sizeof(T)), Raw<T, VEC>::put(o), d.past);
+    } else {
+#pragma unroll
+      for (int s = 0; s < FS; ++s) {
+        float o[VEC];
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          h[e] = fmaf(f[s][e], h[e], b[s][e]);
+          o[e] = t + s < len ? h[e] : 0.0f;
+        }
+        if (p.on && t + s < r1) *at<U>(hp + (int64_t)(t + s) * d.h.step, p.c * sizeof(T)) = Raw<T, VEC>::put(o);
+      }
     }
   }
   if (a.hT != nullptr && p.range == d.ranges - 1 && p.wave == 0 && p.on)
@@ -317,7 +337,7 @@ __global__ __launch_bounds__(64 * NW) void scan_bwd_sum_kernel(Dims d, ScanArgs 
       Raw<T, VEC>::get(rg[s], v);
       Raw<T, VEC>::get(rd[s], g[s]);
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) gate_of(v[e], f[s][e], keep);
+      for (int e = 0; e < VEC; ++e) gate_of<T>(v[e], f[s][e], keep);
     }
     if (t > t0) {
       load_steps<T, VEC, BS>(rg, a.gate, d.gate, p.b, t - BS, len, p.cc, U(0));
@@ -395,13 +415,17 @@ __global__ __launch_bounds__(64 * NW) void scan_bwd_kernel(Dims d, ScanArgs a) {
       Raw<T, VEC>::get(rx[s], x[s]);
       Raw<T, VEC>::get(rd[s], g[s]);
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) gate_of(v[e], f[s][e], keep[s][e]);
-      if (t + s >= len)
+      for (int e = 0; e < VEC; ++e) gate_of<T>(v[e], f[s][e], keep[s][e]);
+    }
+    if (t + BS > len) {
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-          f[s][e] = 1.0f;
-          keep[s][e] = x[s][e] = g[s][e] = 0.0f;
-        }
+      for (int s = 0; s < BS; ++s)
+        if (t + s >= len)
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) {
+            f[s][e] = 1.0f;
+            keep[s][e] = x[s][e] = g[s][e] = 0.0f;
+          }
     }
 #pragma unroll
     for (int e = 0; e < VEC; ++e) h[e] = state[e];
