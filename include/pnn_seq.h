@@ -23,8 +23,8 @@
  *   - Empty problems are valid (pointers of tensors without elements may be NULL).
  *   - Results do not depend on timing: no sum is formed in an order that varies from run to run.
  *   - Return value: PNN_OK or a negative pnn_status; on error nothing has been enqueued, except for
- *     PNN_ERR_HIP.  PNN_ERR_TOO_LARGE: sizes or offsets beyond what the kernels index (2^28 tokens or
- *     samples, 2^23 elements of a table row, 2^31 - 1 classes, 2^30 steps, 2^21 times 64 channels in a
+ *     PNN_ERR_HIP.  PNN_ERR_TOO_LARGE: sizes or offsets beyond what the kernels index (2^28 samples,
+ *     2^23 pieces of 32 tokens x 64 elements or of 32 table rows, 2^31 - 1 classes, 2^30 steps, 2^21 times 64 channels in a
  *     batch, 2^60 elements from a tensor's first to its last).
  */
 #ifndef PNN_SEQ_H

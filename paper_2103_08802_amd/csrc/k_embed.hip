@@ -6,6 +6,7 @@
 // threads each, whatever the tokens' distribution, and the runs that cross tiles are joined from the
 // tiles' partial rows in a second launch, in tile order.  No floating-point atomics.
 #include "device_common.h"
+#include "seq_device.h"
 #include "seq_internal.h"
 
 namespace pnn {
@@ -33,13 +34,15 @@ __device__ __forceinline__ void load_ve(const void* p, int64_t i, float* v) {
     }
   }
 }
+// the same to memory; `past`: see store_to
 template <typename T, int VE>
-__device__ __forceinline__ void store_ve(void* p, int64_t i, const float* v) {
+__device__ __forceinline__ void store_ve(void* p, int64_t i, const float* v, bool past = false) {
   if constexpr (VE == 1) {
-    St<T>::st(p, i, v[0]);
+    if constexpr (sizeof(T) == 4) store_to((float*)p + i, v[0], past);
+    else store_to((uint16_t*)p + i, f2bf(v[0]), past);
   } else {
 #pragma unroll
-    for (int c = 0; c < VE / St<T>::VE; ++c) store_chunk<T>(p, i + c * St<T>::VE, v + c * St<T>::VE);
+    for (int c = 0; c < VE; c += St<T>::VE) store_piece<T>(p, i + c, v + c, past);
   }
 }
 
@@ -56,7 +59,7 @@ struct EmbedFwd {
   const void *table, *tokens;
   void* out;
   int64_t n, vocab, table_stride, row_stride;
-  int width, token_bytes, tpr;
+  int width, token_bytes, tpr, past;
   float scale;
 };
 
@@ -77,7 +80,7 @@ __global__ __launch_bounds__(THREADS) void embed_fwd_kernel(EmbedFwd a) {
 #pragma unroll
         for (int e = 0; e < VE; ++e) v[e] = t < 0 ? 0.0f : __builtin_nanf("");
       }
-      store_ve<TO, VE>(a.out, i * a.row_stride + c, v);
+      store_ve<TO, VE>(a.out, i * a.row_stride + c, v, a.past);
     }
   }
 }
@@ -93,29 +96,49 @@ struct EmbedSort {
   unsigned* hist;              // [blocks][EMB_BINS] of this pass
   unsigned* total;             // [EMB_BINS]: if not NULL, hist holds sums over the earlier workgroups and this all of them
   unsigned* hist_next;         // of the next pass, zero before this launch; NULL: last pass
-  int64_t n, vocab, blocks;
-  int token_bytes, shift;
+  unsigned* present;           // a bit for every row of the table, cleared by the first launch (embed_sum_kernel sets them)
+  int64_t n, vocab, blocks, words;
+  int token_bytes, shift, passes;
 };
 
-__device__ __forceinline__ int32_t sort_key(const EmbedSort& a, int64_t i) {
-  if (a.tokens == nullptr) return a.key_in[i];
-  const int64_t t = token_at(a.tokens, a.token_bytes, i);
-  return t >= 0 && t < a.vocab ? (int32_t)t : (int32_t)a.vocab;
+// key and position of item i; past the end the last one's (not to be used)
+template <bool FIRST>
+__device__ __forceinline__ void item(const EmbedSort& a, int64_t i, int32_t& key, int32_t& pos) {
+  i = i < a.n ? i : a.n - 1;
+  if constexpr (FIRST) {
+    const int64_t t = token_at(a.tokens, a.token_bytes, i);
+    key = t >= 0 && t < a.vocab ? (int32_t)t : (int32_t)a.vocab;
+    pos = (int32_t)i;
+  } else {
+    key = a.key_in[i];
+    pos = a.pos_in[i];
+  }
 }
 
-// first pass's histogram of each workgroup's EMB_ITEMS tokens; clears the later passes' histograms
-__global__ __launch_bounds__(THREADS) void embed_hist_kernel(EmbedSort a, unsigned* hist, int passes) {
+__device__ __forceinline__ void clear_present(const EmbedSort& a) {
+  for (int64_t w = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; w < a.words; w += (int64_t)gridDim.x * blockDim.x)
+    a.present[w] = 0;
+}
+
+// first pass's histogram of each workgroup's EMB_ITEMS tokens; clears the later passes' and the row bits
+__global__ __launch_bounds__(THREADS) void embed_hist_kernel(EmbedSort a) {
   __shared__ unsigned cnt[EMB_BINS];
+  clear_present(a);
+  if (blockIdx.x >= a.blocks) return;
   for (int b = threadIdx.x; b < EMB_BINS; b += THREADS) cnt[b] = 0;
   __syncthreads();
   const int64_t i0 = (int64_t)blockIdx.x * EMB_ITEMS;
-  for (int k = threadIdx.x; k < EMB_ITEMS; k += THREADS)
-    if (i0 + k < a.n) atomicAdd(&cnt[sort_key(a, i0 + k) & (EMB_BINS - 1)], 1u);
+  int32_t key[EMB_ITEMS / THREADS], pos;
+#pragma unroll
+  for (int r = 0; r < EMB_ITEMS / THREADS; ++r) item<true>(a, i0 + r * THREADS + threadIdx.x, key[r], pos);
+#pragma unroll
+  for (int r = 0; r < EMB_ITEMS / THREADS; ++r)
+    if (i0 + r * THREADS + threadIdx.x < a.n) atomicAdd(&cnt[key[r] & (EMB_BINS - 1)], 1u);
   __syncthreads();
   for (int b = threadIdx.x; b < EMB_BINS; b += THREADS) {
-    unsigned* h = hist + (int64_t)blockIdx.x * EMB_BINS + b;
+    unsigned* h = a.hist + (int64_t)blockIdx.x * EMB_BINS + b;
     h[0] = cnt[b];
-    for (int p = 1; p < passes; ++p) h[p * a.blocks * EMB_BINS] = 0;
+    for (int p = 1; p < a.passes; ++p) h[p * a.blocks * EMB_BINS] = 0;
   }
 }
 
@@ -128,6 +151,7 @@ __global__ __launch_bounds__(THREADS) void embed_offset_kernel(EmbedSort a) {
   const int64_t b1 = b0 + share < a.blocks ? b0 + share : a.blocks;
   __shared__ unsigned sum[32][8];
   unsigned t = 0;
+#pragma unroll 8
   for (int64_t b = b0; b < b1; ++b) t += a.hist[b * EMB_BINS + bin];
   sum[part][threadIdx.x & 7] = t;
   __syncthreads();
@@ -136,6 +160,7 @@ __global__ __launch_bounds__(THREADS) void embed_offset_kernel(EmbedSort a) {
     if (p < part) o += sum[p][threadIdx.x & 7];
     all += sum[p][threadIdx.x & 7];
   }
+#pragma unroll 8
   for (int64_t b = b0; b < b1; ++b) {
     const unsigned c = a.hist[b * EMB_BINS + bin];
     a.hist[b * EMB_BINS + bin] = o;
@@ -144,26 +169,80 @@ __global__ __launch_bounds__(THREADS) void embed_offset_kernel(EmbedSort a) {
   if (part == 0) a.total[bin] = all;
 }
 
+// Lanes of the wave whose item has the same digit (ballots over its bits), among those that are on.
+__device__ __forceinline__ unsigned long long same_digit(int digit, bool on) {
+  unsigned long long same = __ballot(on);
+#pragma unroll
+  for (int b = 0; b < EMB_DIGIT; ++b) {
+    const unsigned long long m = __ballot((digit >> b) & 1);
+    same &= ((digit >> b) & 1) ? m : ~m;
+  }
+  return same;
+}
+
+// The place of each lane's item: the counter of its digit plus its rank among the wave's equal digits.
+// The counters belong to this wave; the first lane of each group advances its counter once every lane
+// has read (one wave's LDS operations complete in order; the fences keep the compiler to it).
+__device__ __forceinline__ unsigned take_place(unsigned* counter, int digit, bool on) {
+  const unsigned long long same = same_digit(digit, on);
+  const int rank = __popcll(same & ((1ull << (threadIdx.x & 63)) - 1));
+  unsigned at = 0;
+  if (on) at = counter[digit];
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  if (on && rank == 0) counter[digit] = at + __popcll(same);
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  return at + rank;
+}
+
+// Turns the waves' digit counts cnt[wave][bin] into first places: behind the smaller digits of all
+// items (tot: the counts over all items of this thread's bins, BPT of them in a row), behind `before` (equal digits of earlier
+// workgroups), behind earlier waves.
+template <int NW, int BPT>
+__device__ __forceinline__ void first_places(unsigned (*cnt)[EMB_BINS], const unsigned* tot, const unsigned* before,
+                                             unsigned* wsum) {
+  const int tid = threadIdx.x, wave = tid / 64, lane = tid & 63;
+  unsigned own = 0;
+#pragma unroll
+  for (int k = 0; k < BPT; ++k) own += tot[k];
+  unsigned inc = own;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const unsigned up = __shfl_up(inc, o, 64);
+    if (lane >= o) inc += up;
+  }
+  if (lane == 63) wsum[wave] = inc;
+  __syncthreads();             // also: every wave's counts are complete
+  unsigned start = inc - own;
+  for (int w = 0; w < wave; ++w) start += wsum[w];
+#pragma unroll
+  for (int k = 0; k < BPT; ++k) {
+    unsigned o = start + before[k];
+    for (int w = 0; w < NW; ++w) {
+      const unsigned c = cnt[w][BPT * tid + k];
+      cnt[w][BPT * tid + k] = o;
+      o += c;
+    }
+    start += tot[k];
+  }
+  __syncthreads();
+}
+
 // One stable radix pass: workgroup b places its EMB_ITEMS items behind those of smaller digits and
 // those of the same digit in earlier workgroups.  Within the workgroup each wave owns a contiguous
-// quarter; a first sweep counts its digits, a second one ranks items by the number of equal digits
-// in lower lanes (ballots) and in earlier rounds (the wave's counters).  Integer counts only, so the
+// quarter: it counts its digits, then places its items 64 at a time.  Integer counts only, so the
 // atomics on the next pass's histogram do not depend on their order.
+template <bool FIRST>
 __global__ __launch_bounds__(THREADS) void embed_scatter_kernel(EmbedSort a) {
   constexpr int WAVES = THREADS / 64, ROUNDS = EMB_ITEMS / THREADS;
   __shared__ unsigned base[WAVES][EMB_BINS];
   __shared__ unsigned wsum[WAVES];
   const int tid = threadIdx.x, wave = tid / 64, lane = tid & 63;
-  for (int b = tid; b < WAVES * EMB_BINS; b += THREADS) (&base[0][0])[b] = 0;
-  __syncthreads();
-  const int64_t i0 = (int64_t)blockIdx.x * EMB_ITEMS + wave * (EMB_ITEMS / WAVES);
-  int32_t key[ROUNDS];
+  const int64_t i0 = (int64_t)blockIdx.x * EMB_ITEMS + wave * (EMB_ITEMS / WAVES) + lane;
+  int32_t key[ROUNDS], pos[ROUNDS];
 #pragma unroll
-  for (int r = 0; r < ROUNDS; ++r) {
-    const int64_t i = i0 + r * 64 + lane;
-    key[r] = i < a.n ? sort_key(a, i) : -1;
-    if (i < a.n) atomicAdd(&base[wave][(key[r] >> a.shift) & (EMB_BINS - 1)], 1u);
-  }
+  for (int r = 0; r < ROUNDS; ++r) item<FIRST>(a, i0 + r * 64, key[r], pos[r]);
   // each thread: two neighbouring bins; their counts over all workgroups, and over earlier ones
   static_assert(EMB_BINS == 2 * THREADS, "two bins a thread");
   unsigned tot[2] = {0, 0}, before[2] = {0, 0};
@@ -173,65 +252,85 @@ __global__ __launch_bounds__(THREADS) void embed_scatter_kernel(EmbedSort a) {
     before[1] = h.y;
     tot[0] = t.x;
     tot[1] = t.y;
-  } else for (int64_t b = 0; b < a.blocks; ++b) {
-    const uint2 h = ((const uint2*)(a.hist + b * EMB_BINS))[tid];
-    tot[0] += h.x;
-    tot[1] += h.y;
-    if (b < blockIdx.x) {
-      before[0] += h.x;
-      before[1] += h.y;
+  } else {
+#pragma unroll 8
+    for (int b = 0; b < (int)a.blocks; ++b) {
+      const uint2 h = ((const uint2*)(a.hist + b * EMB_BINS))[tid];
+      tot[0] += h.x;
+      tot[1] += h.y;
+      before[0] += b < (int)blockIdx.x ? h.x : 0;
+      before[1] += b < (int)blockIdx.x ? h.y : 0;
     }
   }
-  // exclusive sum of the totals over the bins
-  unsigned inc = tot[0] + tot[1];
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const unsigned up = __shfl_up(inc, o, 64);
-    if (lane >= o) inc += up;
-  }
-  if (lane == 63) wsum[wave] = inc;
-  __syncthreads();             // also: every wave's digit counts are complete
-  unsigned start = inc - tot[0] - tot[1];
-  for (int w = 0; w < wave; ++w) start += wsum[w];
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    unsigned o = start + before[k];
-    for (int w = 0; w < WAVES; ++w) {
-      const unsigned c = base[w][2 * tid + k];
-      base[w][2 * tid + k] = o;
-      o += c;
-    }
-    start += tot[k];
-  }
+  for (int b = tid; b < WAVES * EMB_BINS; b += THREADS) (&base[0][0])[b] = 0;
   __syncthreads();
-  // The wave's counters are only touched by its own lanes from here on; the leader of each group of
-  // equal digits advances them, after every lane of the round has read its own.
-  for (int r = 0; r < ROUNDS; ++r) {
-    const int64_t i = i0 + r * 64 + lane;
-    const bool on = i < a.n;
-    const int digit = (key[r] >> a.shift) & (EMB_BINS - 1);
-    unsigned long long same = __ballot(on);
 #pragma unroll
-    for (int b = 0; b < EMB_DIGIT; ++b) {
-      const unsigned long long m = __ballot((digit >> b) & 1);
-      same &= ((digit >> b) & 1) ? m : ~m;
-    }
-    const int rank = __popcll(same & ((1ull << lane) - 1));
-    unsigned at = 0;
-    if (on) at = base[wave][digit];
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    if (on && rank == 0) base[wave][digit] = at + __popcll(same);
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    if (on) {
-      const unsigned to = at + rank;
-      a.key_out[to] = key[r];
-      a.pos_out[to] = a.tokens != nullptr ? (int32_t)i : a.pos_in[i];
-      if (a.hist_next != nullptr)
-        atomicAdd(&a.hist_next[(int64_t)(to / EMB_ITEMS) * EMB_BINS + ((key[r] >> (a.shift + EMB_DIGIT)) & (EMB_BINS - 1))], 1u);
-    }
+  for (int r = 0; r < ROUNDS; ++r)
+    if (i0 + r * 64 < a.n) atomicAdd(&base[wave][(key[r] >> a.shift) & (EMB_BINS - 1)], 1u);
+  first_places<WAVES, 2>(base, tot, before, wsum);
+#pragma unroll
+  for (int r = 0; r < ROUNDS; ++r) {
+    const bool on = i0 + r * 64 < a.n;
+    const unsigned to = take_place(base[wave], (key[r] >> a.shift) & (EMB_BINS - 1), on);
+    if (!on) continue;
+    a.key_out[to] = key[r];
+    a.pos_out[to] = pos[r];
+    if (a.hist_next != nullptr)
+      atomicAdd(&a.hist_next[(int64_t)(to / EMB_ITEMS) * EMB_BINS + ((key[r] >> (a.shift + EMB_DIGIT)) & (EMB_BINS - 1))], 1u);
   }
+}
+
+// Up to EMB_ITEMS tokens: every pass in one workgroup, the items in LDS between passes.
+__global__ __launch_bounds__(2 * THREADS) void embed_sort_kernel(EmbedSort a) {
+  constexpr int WAVES = 2 * THREADS / 64, ROUNDS = EMB_ITEMS / (2 * THREADS);
+  __shared__ unsigned base[WAVES][EMB_BINS];
+  __shared__ unsigned wsum[WAVES];
+  __shared__ int32_t skey[EMB_ITEMS], spos[EMB_ITEMS];
+  clear_present(a);
+  if (blockIdx.x > 0) return;
+  const int tid = threadIdx.x, wave = tid / 64, lane = tid & 63;
+  const int i0 = wave * (EMB_ITEMS / WAVES) + lane, n = (int)a.n;
+  int32_t key[ROUNDS], pos[ROUNDS];
+#pragma unroll
+  for (int r = 0; r < ROUNDS; ++r) item<true>(a, i0 + r * 64, key[r], pos[r]);
+  for (int p = 0; p < a.passes; ++p) {
+    const int shift = p * EMB_DIGIT;
+    for (int b = tid; b < WAVES * EMB_BINS; b += 2 * THREADS) (&base[0][0])[b] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r)
+      if (i0 + r * 64 < n) atomicAdd(&base[wave][(key[r] >> shift) & (EMB_BINS - 1)], 1u);
+    __syncthreads();
+    static_assert(EMB_BINS == 2 * THREADS, "a bin a thread");
+    unsigned tot = 0;
+    const unsigned before = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) tot += base[w][tid];
+    first_places<WAVES, 1>(base, &tot, &before, wsum);
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r) {
+      const bool on = i0 + r * 64 < n;
+      const unsigned to = take_place(base[wave], (key[r] >> shift) & (EMB_BINS - 1), on);
+      if (on) {
+        skey[to] = key[r];
+        spos[to] = pos[r];
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r)
+      if (i0 + r * 64 < n) {
+        key[r] = skey[i0 + r * 64];
+        pos[r] = spos[i0 + r * 64];
+      }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int r = 0; r < ROUNDS; ++r)
+    if (i0 + r * 64 < n) {
+      a.key_out[i0 + r * 64] = key[r];
+      a.pos_out[i0 + r * 64] = pos[r];
+    }
 }
 
 // ---- sums -------------------------------------------------------------------------------------
@@ -240,8 +339,10 @@ struct EmbedSum {
   const int32_t *key, *pos;    // sorted
   const void* dout;
   float *dtable, *part;        // part [tiles][2][width]
+  unsigned* present;           // NULL: no row has tokens
   int64_t n, vocab, tiles, table_stride, row_stride;
-  int width, tpr, accumulate;
+  int64_t join_blocks;         // second launch: workgroups that join runs; the others clear rows
+  int width, tpr, accumulate, past;
   float scale;
 };
 
@@ -257,14 +358,17 @@ __device__ __forceinline__ void write_row(const EmbedSum& a, int64_t row, int c,
 #pragma unroll
     for (int e = 0; e < VE; ++e) v[e] += old[e];
   }
-  store_ve<float, VE>(a.dtable, o, v);
+  store_ve<float, VE>(a.dtable, o, v, a.past);
 }
 
 // Sums of one tile: runs inside the tile are written, a run from the tile before goes to part row 0
-// (also when it goes on behind this tile), one that starts here and goes on to part row 1.
-template <typename T, int VE>
+// (also when it goes on behind this tile), one that starts here and goes on to part row 1.  The rows
+// of eight positions are loaded at a time.  UNI: a tile's threads are whole waves.
+template <typename T, int VE, bool UNI>
 __global__ __launch_bounds__(THREADS) void embed_sum_kernel(EmbedSum a) {
-  const int64_t tile = (int64_t)blockIdx.x * (THREADS / a.tpr) + threadIdx.x / a.tpr;
+  int sub = threadIdx.x / a.tpr;
+  if constexpr (UNI) sub = __builtin_amdgcn_readfirstlane(sub);
+  const int64_t tile = (int64_t)blockIdx.x * (THREADS / a.tpr) + sub;
   const int c = ((threadIdx.x & (a.tpr - 1)) + blockIdx.y * a.tpr) * VE;
   if (tile >= a.tiles || c >= a.width) return;
   const int64_t s0 = tile * EMB_RUN, s1 = s0 + EMB_RUN < a.n ? s0 + EMB_RUN : a.n;
@@ -275,66 +379,104 @@ __global__ __launch_bounds__(THREADS) void embed_sum_kernel(EmbedSum a) {
   for (int e = 0; e < VE; ++e) acc[e] = 0.0f;
   auto flush = [&](bool at_end) {
     if (cur >= a.vocab) return;
-    if (cur == prev) store_ve<float, VE>(a.part, tile * 2 * a.width + c, acc);
-    else if (at_end && cur == next) store_ve<float, VE>(a.part, (tile * 2 + 1) * a.width + c, acc);
-    else write_row<VE>(a, cur, c, acc);
-  };
-  for (int64_t s = s0; s < s1; ++s) {
-    const int32_t k = a.key[s];
-    if (k != cur) {
-      flush(false);
-      cur = k;
-#pragma unroll
-      for (int e = 0; e < VE; ++e) acc[e] = 0.0f;
+    if (cur == prev) {
+      store_ve<float, VE>(a.part, tile * 2 * a.width + c, acc);
+    } else {
+      if (c == 0 && !a.accumulate) atomicOr(&a.present[cur >> 5], 1u << (cur & 31));
+      if (at_end && cur == next) store_ve<float, VE>(a.part, (tile * 2 + 1) * a.width + c, acc);
+      else write_row<VE>(a, cur, c, acc);
     }
-    if (k >= a.vocab) return;
-    float v[VE];
-    load_ve<T, VE>(a.dout, (int64_t)a.pos[s] * a.row_stride + c, v);
+  };
+  constexpr int U = 8;
+  for (int64_t s = s0; s < s1 && cur < a.vocab; s += U) {
+    int32_t k[U], p[U];
+    float v[U][VE];
 #pragma unroll
-    for (int e = 0; e < VE; ++e) acc[e] += v[e];
+    for (int u = 0; u < U; ++u) {
+      const int64_t i = s + u < s1 ? s + u : s1 - 1;
+      k[u] = a.key[i];
+      p[u] = a.pos[i];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) load_ve<T, VE>(a.dout, (int64_t)p[u] * a.row_stride + c, v[u]);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (s + u >= s1) break;
+      if (k[u] != cur) {
+        flush(false);
+        cur = k[u];
+#pragma unroll
+        for (int e = 0; e < VE; ++e) acc[e] = 0.0f;
+      }
+#pragma unroll
+      for (int e = 0; e < VE; ++e) acc[e] += v[u][e];
+    }
   }
   flush(true);
 }
 
-// Runs over several tiles, by the tile they start in: its part row 1, then the part rows 0 of the
-// tiles up to the one the run ends in.
+// Second launch.  Its first join_blocks workgroups join the runs over several tiles, by the tile they
+// start in: its part row 1, then the part rows 0 of the tiles up to the one the run ends in; each of
+// the JW groups of 64 threads takes every JW-th of them, the groups' sums are added in order.  The
+// others clear the rows without tokens, 32 (a word of `present`) each.
 template <int VE>
 __global__ __launch_bounds__(THREADS) void embed_join_kernel(EmbedSum a) {
-  const int64_t tile = (int64_t)blockIdx.x * (THREADS / a.tpr) + threadIdx.x / a.tpr;
-  const int c = ((threadIdx.x & (a.tpr - 1)) + blockIdx.y * a.tpr) * VE;
-  if (tile + 1 >= a.tiles || c >= a.width) return;
-  const int64_t s0 = tile * EMB_RUN, s1 = s0 + EMB_RUN;
-  const int32_t cur = a.key[s1];
-  if (cur >= a.vocab || a.key[s1 - 1] != cur || (s0 > 0 && a.key[s0 - 1] == cur)) return;
-  float acc[VE];
-  load_ve<float, VE>(a.part, (tile * 2 + 1) * a.width + c, acc);
-  for (int64_t t = tile + 1; t < a.tiles && a.key[t * EMB_RUN] == cur; ++t) {
-    // the run reaches tile t: at its first position the token still is this one
-    float v[VE];
-    load_ve<float, VE>(a.part, t * 2 * a.width + c, v);
-#pragma unroll
-    for (int e = 0; e < VE; ++e) acc[e] += v[e];
-  }
-  write_row<VE>(a, cur, c, acc);
-}
-
-// Rows without tokens: zero (not when the gradient is added to).  A row has tokens if the sorted keys hold it.
-template <int VE>
-__global__ __launch_bounds__(THREADS) void embed_zero_kernel(EmbedSum a) {
-  const int rows = THREADS / a.tpr;
-  const int lane = threadIdx.x & (a.tpr - 1);
-  for (int64_t v = (int64_t)blockIdx.x * rows + threadIdx.x / a.tpr; v < a.vocab; v += (int64_t)gridDim.x * rows) {
-    int64_t lo = 0, hi = a.n;
+  constexpr int JW = THREADS / 64;
+  if (blockIdx.x < a.join_blocks) {
+    __shared__ float sum[JW][64][VE];
+    const int slabs = (a.width + 64 * VE - 1) / (64 * VE);
+    const int64_t tile = blockIdx.x / slabs;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int c = ((int)(blockIdx.x - tile * slabs) * 64 + lane) * VE;
+    const int64_t s0 = tile * EMB_RUN, s1 = s0 + EMB_RUN;
+    const int32_t cur = a.key[s1];
+    if (cur >= a.vocab || a.key[s1 - 1] != cur || (s0 > 0 && a.key[s0 - 1] == cur)) return;
+    // the run's last tile: the last one whose first key is this token
+    int64_t lo = tile + 1, hi = a.tiles - 1;
     while (lo < hi) {
-      const int64_t mid = (lo + hi) >> 1;
-      if (a.key[mid] < v) lo = mid + 1;
-      else hi = mid;
+      const int64_t mid = (lo + hi + 1) >> 1;
+      if (a.key[mid * EMB_RUN] == cur) lo = mid;
+      else hi = mid - 1;
     }
-    if (lo < a.n && a.key[lo] == v) continue;
-    float z[VE];
+    const bool on = c < a.width;
+    float acc[VE];
 #pragma unroll
-    for (int e = 0; e < VE; ++e) z[e] = 0.0f;
-    for (int c = lane * VE; c < a.width; c += a.tpr * VE) store_ve<float, VE>(a.dtable, v * a.table_stride + c, z);
+    for (int e = 0; e < VE; ++e) acc[e] = 0.0f;
+    // rows of the sum: 0 is the first tile's part row 1, r >= 1 part row 0 of tile + r
+    const int64_t rows = lo - tile + 1;
+    constexpr int U = 4;
+    for (int64_t r = wave; on && r < rows; r += U * JW) {
+      float v[U][VE];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int64_t i = r + u * JW < rows ? r + u * JW : r;
+        load_ve<float, VE>(a.part, (i == 0 ? tile * 2 + 1 : (tile + i) * 2) * a.width + c, v[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (r + u * JW < rows)
+#pragma unroll
+          for (int e = 0; e < VE; ++e) acc[e] += v[u][e];
+    }
+#pragma unroll
+    for (int e = 0; e < VE; ++e) sum[wave][lane][e] = acc[e];
+    __syncthreads();
+    if (wave != 0 || !on) return;
+#pragma unroll
+    for (int w = 1; w < JW; ++w)
+#pragma unroll
+      for (int e = 0; e < VE; ++e) acc[e] += sum[w][lane][e];
+    write_row<VE>(a, cur, c, acc);
+    return;
+  }
+  const int64_t word = blockIdx.x - a.join_blocks;
+  const unsigned has = a.present != nullptr ? a.present[word] : 0;
+  const float z[VE] = {};
+  const int rows = THREADS / a.tpr, lane = threadIdx.x & (a.tpr - 1);
+  for (int r = threadIdx.x / a.tpr; r < 32; r += rows) {
+    const int64_t v = word * 32 + r;
+    if (v >= a.vocab || (has >> r & 1)) continue;
+    for (int c = lane * VE; c < a.width; c += a.tpr * VE) store_ve<float, VE>(a.dtable, v * a.table_stride + c, z, a.past);
   }
 }
 
@@ -354,6 +496,7 @@ int launch_embed_fwd(const pnn_embed_desc& d, const void* table, const void* tok
   a.width = (int)d.width;
   a.token_bytes = d.token_bytes;
   a.scale = d.scale;
+  a.past = d.n * d.width * (d.dtype == PNN_F32 ? 4 : 2) > L2_BYTES;
   const int es = d.dtype == PNN_F32 ? 4 : 2, et = d.table_dtype == PNN_F32 ? 4 : 2;
   // 8 elements a piece: whole 16-byte pieces on both sides
   const bool wide = d.width % 8 == 0 && al16p(table) && al16p(out) && d.table_stride * et % 16 == 0 && d.row_stride * es % 16 == 0;
@@ -377,40 +520,50 @@ int launch_embed_bwd(const pnn_embed_desc& d, const void* dout, const void* toke
                      void* ws, hipStream_t s) {
   const EmbedWs w = embed_ws(d);
   char* base = (char*)ws;
+  const dim3 block(THREADS);
   EmbedSort a;
   a.n = d.n;
   a.vocab = d.vocab;
   a.blocks = w.blocks;
   a.token_bytes = d.token_bytes;
-  unsigned* hist = (unsigned*)(base + w.hist);
-  for (int p = 0; d.n > 0 && p < w.passes; ++p) {
-    a.tokens = p == 0 ? tokens : nullptr;
-    a.key_in = (const int32_t*)(base + w.key[(p + 1) & 1]);
-    a.pos_in = (const int32_t*)(base + w.pos[(p + 1) & 1]);
-    a.key_out = (int32_t*)(base + w.key[p & 1]);
-    a.pos_out = (int32_t*)(base + w.pos[p & 1]);
-    a.hist = hist + p * w.blocks * EMB_BINS;
-    a.hist_next = p + 1 < w.passes ? hist + (p + 1) * w.blocks * EMB_BINS : nullptr;
-    a.shift = p * EMB_DIGIT;
-    if (p == 0) {
-      hipLaunchKernelGGL(embed_hist_kernel, dim3((unsigned)w.blocks), dim3(THREADS), 0, s, a, hist, w.passes);
-      if (const hipError_t e = hipGetLastError()) return (int)e;
-    }
-    a.total = nullptr;
-    if (w.blocks > EMB_DIRECT) {
-      a.total = (unsigned*)(base + w.total);
-      hipLaunchKernelGGL(embed_offset_kernel, dim3(EMB_BINS / 8), dim3(THREADS), 0, s, a);
-      if (const hipError_t e = hipGetLastError()) return (int)e;
-    }
-    hipLaunchKernelGGL(embed_scatter_kernel, dim3((unsigned)w.blocks), dim3(THREADS), 0, s, a);
+  a.passes = w.passes;
+  a.words = accumulate ? 0 : w.words;
+  a.present = (unsigned*)(base + w.present);
+  // launches that clear the row bits: a workgroup for at most 4096 words more
+  const int64_t clear = cdiv64(a.words, 4096) < MAX_GRID ? cdiv64(a.words, 4096) : MAX_GRID;
+  int out = 0;
+  if (d.n > 0 && w.blocks == 1) {
+    a.tokens = tokens;
+    a.key_out = (int32_t*)(base + w.key[0]);
+    a.pos_out = (int32_t*)(base + w.pos[0]);
+    hipLaunchKernelGGL(embed_sort_kernel, dim3((unsigned)(clear > 1 ? clear : 1)), dim3(2 * THREADS), 0, s, a);
     if (const hipError_t e = hipGetLastError()) return (int)e;
+  } else if (d.n > 0) {
+    a.tokens = tokens;
+    for (int p = 0; p < w.passes; ++p) {
+      out = p & 1;
+      a.key_in = (const int32_t*)(base + w.key[1 - out]);
+      a.pos_in = (const int32_t*)(base + w.pos[1 - out]);
+      a.key_out = (int32_t*)(base + w.key[out]);
+      a.pos_out = (int32_t*)(base + w.pos[out]);
+      a.hist = (unsigned*)(base + w.hist) + p * w.blocks * EMB_BINS;
+      a.hist_next = p + 1 < w.passes ? a.hist + w.blocks * EMB_BINS : nullptr;
+      a.total = w.blocks > EMB_DIRECT ? (unsigned*)(base + w.total) : nullptr;
+      a.shift = p * EMB_DIGIT;
+      if (p == 0) hipLaunchKernelGGL(embed_hist_kernel, dim3((unsigned)(clear > w.blocks ? clear : w.blocks)), block, 0, s, a);
+      if (a.total != nullptr) hipLaunchKernelGGL(embed_offset_kernel, dim3(EMB_BINS / 8), block, 0, s, a);
+      if (p == 0) hipLaunchKernelGGL(embed_scatter_kernel<true>, dim3((unsigned)w.blocks), block, 0, s, a);
+      else hipLaunchKernelGGL(embed_scatter_kernel<false>, dim3((unsigned)w.blocks), block, 0, s, a);
+      if (const hipError_t e = hipGetLastError()) return (int)e;
+    }
   }
   EmbedSum m;
-  m.key = (const int32_t*)(base + w.key[(w.passes + 1) & 1]);
-  m.pos = (const int32_t*)(base + w.pos[(w.passes + 1) & 1]);
+  m.key = (const int32_t*)(base + w.key[out]);
+  m.pos = (const int32_t*)(base + w.pos[out]);
   m.dout = dout;
   m.dtable = dtable;
   m.part = (float*)(base + w.part);
+  m.present = d.n > 0 ? a.present : nullptr;
   m.n = d.n;
   m.vocab = d.vocab;
   m.tiles = w.tiles;
@@ -418,18 +571,18 @@ int launch_embed_bwd(const pnn_embed_desc& d, const void* dout, const void* toke
   m.row_stride = d.row_stride;
   m.width = (int)d.width;
   m.accumulate = accumulate != 0;
+  m.past = d.vocab * d.width * 4 > L2_BYTES;
   m.scale = d.scale;
   const int es = d.dtype == PNN_F32 ? 4 : 2;
   const bool wide = d.width % 8 == 0 && al16p(dtable) && al16p(dout) && d.table_stride % 4 == 0 && d.row_stride * es % 16 == 0;
   const int64_t pieces = wide ? d.width / 8 : d.width;
   m.tpr = threads_per_row(pieces);
-  const dim3 block(THREADS);
   if (d.n > 0) {
     const dim3 grid((unsigned)cdiv64(w.tiles, THREADS / m.tpr), (unsigned)cdiv64(pieces, m.tpr));
-#define SUMS(T, VE)                                                        \
-  do {                                                                     \
-    hipLaunchKernelGGL((embed_sum_kernel<T, VE>), grid, block, 0, s, m);   \
-    hipLaunchKernelGGL((embed_join_kernel<VE>), grid, block, 0, s, m);     \
+#define SUMS(T, VE)                                                                                    \
+  do {                                                                                                 \
+    if (m.tpr >= 64) hipLaunchKernelGGL((embed_sum_kernel<T, VE, true>), grid, block, 0, s, m);        \
+    else hipLaunchKernelGGL((embed_sum_kernel<T, VE, false>), grid, block, 0, s, m);                   \
   } while (0)
     if (es == 4) {
       if (wide) SUMS(float, 8);
@@ -441,12 +594,11 @@ int launch_embed_bwd(const pnn_embed_desc& d, const void* dout, const void* toke
 #undef SUMS
     if (const hipError_t e = hipGetLastError()) return (int)e;
   }
-  if (!m.accumulate) {
-    const int64_t g = cdiv64(d.vocab, THREADS / m.tpr);
-    const dim3 grid((unsigned)(g < MAX_GRID ? g : MAX_GRID));
-    if (wide) hipLaunchKernelGGL((embed_zero_kernel<8>), grid, block, 0, s, m);
-    else hipLaunchKernelGGL((embed_zero_kernel<1>), grid, block, 0, s, m);
-  }
+  m.join_blocks = (w.tiles > 1 ? w.tiles - 1 : 0) * cdiv64(d.width, 64 * (wide ? 8 : 1));
+  const int64_t blocks = m.join_blocks + (m.accumulate ? 0 : w.words);
+  if (blocks == 0) return 0;
+  if (wide) hipLaunchKernelGGL((embed_join_kernel<8>), dim3((unsigned)blocks), block, 0, s, m);
+  else hipLaunchKernelGGL((embed_join_kernel<1>), dim3((unsigned)blocks), block, 0, s, m);
   return (int)hipGetLastError();
 }
 

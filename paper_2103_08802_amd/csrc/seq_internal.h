@@ -25,17 +25,18 @@ inline int embed_passes(int64_t vocab) {
   return (bits + EMB_DIGIT - 1) / EMB_DIGIT;
 }
 // Workspace of the gradient: keys and positions twice (the radix passes go from one to the other),
-// a histogram [workgroup][bin] for every pass, and the partial rows [tile][2][width] of runs that
+// a histogram [workgroup][bin] for every pass and the sums over its workgroups, a bit for every table row, and the partial rows [tile][2][width] of runs that
 // cross tiles.
 struct EmbedWs {
-  int64_t key[2], pos[2], hist, total, part, bytes;
-  int64_t blocks, tiles;
+  int64_t key[2], pos[2], hist, total, present, part, bytes;
+  int64_t blocks, tiles, words;
   int passes;
 };
 inline EmbedWs embed_ws(const pnn_embed_desc& d) {
   EmbedWs w;
   w.blocks = cdiv64(d.n, EMB_ITEMS);
   w.tiles = cdiv64(d.n, EMB_RUN);
+  w.words = cdiv64(d.vocab, 32);
   w.passes = embed_passes(d.vocab);
   int64_t o = 0;
   for (int i = 0; i < 2; ++i) {
@@ -48,6 +49,8 @@ inline EmbedWs embed_ws(const pnn_embed_desc& d) {
   o += round256(w.passes * w.blocks * EMB_BINS * 4);
   w.total = o;
   o += EMB_BINS * 4;
+  w.present = o;
+  o += round256(w.words * 4);
   w.part = o;
   o += round256(w.tiles * 2 * d.width * 4);
   w.bytes = o;
