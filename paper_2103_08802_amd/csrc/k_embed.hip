@@ -2,7 +2,7 @@
 //
 // Forward: out[i] = scale table[tok_i], a gather.  Backward: dtable[v] = scale sum_{tok_i = v} dout[i].
 // The tokens are sorted by a stable radix sort over (token, position), so that every table row's
-// terms stand together in token order; tiles of EMB_RUN sorted positions are summed by one group of
+// terms stand together in token order; tiles of sorted positions are summed by one group of
 // threads each, whatever the tokens' distribution, and the runs that cross tiles are joined from the
 // tiles' partial rows in a second launch, in tile order.  No floating-point atomics.
 #include "device_common.h"
@@ -41,8 +41,9 @@ __device__ __forceinline__ void store_ve(void* p, int64_t i, const float* v, boo
     if constexpr (sizeof(T) == 4) store_to((float*)p + i, v[0], past);
     else store_to((uint16_t*)p + i, f2bf(v[0]), past);
   } else {
+    // past the caches only whole lines: where a thread has one piece, its neighbours have the pieces around it
 #pragma unroll
-    for (int c = 0; c < VE; c += St<T>::VE) store_piece<T>(p, i + c, v + c, past);
+    for (int c = 0; c < VE; c += St<T>::VE) store_piece<T>(p, i + c, v + c, past && VE == St<T>::VE);
   }
 }
 
@@ -93,9 +94,8 @@ struct EmbedSort {
   const void* tokens;          // first pass: keys from the tokens, positions 0, 1, ..
   const int32_t *key_in, *pos_in;
   int32_t *key_out, *pos_out;
-  unsigned* hist;              // [blocks][EMB_BINS] of this pass
+  unsigned* hist;              // [blocks][EMB_BINS]
   unsigned* total;             // [EMB_BINS]: if not NULL, hist holds sums over the earlier workgroups and this all of them
-  unsigned* hist_next;         // of the next pass, zero before this launch; NULL: last pass
   unsigned* present;           // a bit for every row of the table, cleared by the first launch (embed_sum_kernel sets them)
   int64_t n, vocab, blocks, words;
   int token_bytes, shift, passes;
@@ -120,26 +120,25 @@ __device__ __forceinline__ void clear_present(const EmbedSort& a) {
     a.present[w] = 0;
 }
 
-// first pass's histogram of each workgroup's EMB_ITEMS tokens; clears the later passes' and the row bits
+// The pass's histogram of each workgroup's EMB_ITEMS items (the first one also clears the row bits).  A launch of its
+// own for every pass: counted by the pass before as it places its items, the frequent tokens' digits meet in a few
+// counters (16384 tokens: that pass 26 us instead of 7).
+template <bool FIRST>
 __global__ __launch_bounds__(THREADS) void embed_hist_kernel(EmbedSort a) {
   __shared__ unsigned cnt[EMB_BINS];
-  clear_present(a);
+  if (FIRST) clear_present(a);
   if (blockIdx.x >= a.blocks) return;
   for (int b = threadIdx.x; b < EMB_BINS; b += THREADS) cnt[b] = 0;
   __syncthreads();
   const int64_t i0 = (int64_t)blockIdx.x * EMB_ITEMS;
   int32_t key[EMB_ITEMS / THREADS], pos;
 #pragma unroll
-  for (int r = 0; r < EMB_ITEMS / THREADS; ++r) item<true>(a, i0 + r * THREADS + threadIdx.x, key[r], pos);
+  for (int r = 0; r < EMB_ITEMS / THREADS; ++r) item<FIRST>(a, i0 + r * THREADS + threadIdx.x, key[r], pos);
 #pragma unroll
   for (int r = 0; r < EMB_ITEMS / THREADS; ++r)
-    if (i0 + r * THREADS + threadIdx.x < a.n) atomicAdd(&cnt[key[r] & (EMB_BINS - 1)], 1u);
+    if (i0 + r * THREADS + threadIdx.x < a.n) atomicAdd(&cnt[(key[r] >> a.shift) & (EMB_BINS - 1)], 1u);
   __syncthreads();
-  for (int b = threadIdx.x; b < EMB_BINS; b += THREADS) {
-    unsigned* h = a.hist + (int64_t)blockIdx.x * EMB_BINS + b;
-    h[0] = cnt[b];
-    for (int p = 1; p < a.passes; ++p) h[p * a.blocks * EMB_BINS] = 0;
-  }
+  for (int b = threadIdx.x; b < EMB_BINS; b += THREADS) a.hist[(int64_t)blockIdx.x * EMB_BINS + b] = cnt[b];
 }
 
 // hist[b][bin] becomes the sum over the workgroups before b, total[bin] the sum over all: 8 bins a
@@ -231,8 +230,7 @@ __device__ __forceinline__ void first_places(unsigned (*cnt)[EMB_BINS], const un
 
 // One stable radix pass: workgroup b places its EMB_ITEMS items behind those of smaller digits and
 // those of the same digit in earlier workgroups.  Within the workgroup each wave owns a contiguous
-// quarter: it counts its digits, then places its items 64 at a time.  Integer counts only, so the
-// atomics on the next pass's histogram do not depend on their order.
+// quarter: it counts its digits, then places its items 64 at a time.
 template <bool FIRST>
 __global__ __launch_bounds__(THREADS) void embed_scatter_kernel(EmbedSort a) {
   constexpr int WAVES = THREADS / 64, ROUNDS = EMB_ITEMS / THREADS;
@@ -275,8 +273,6 @@ __global__ __launch_bounds__(THREADS) void embed_scatter_kernel(EmbedSort a) {
     if (!on) continue;
     a.key_out[to] = key[r];
     a.pos_out[to] = pos[r];
-    if (a.hist_next != nullptr)
-      atomicAdd(&a.hist_next[(int64_t)(to / EMB_ITEMS) * EMB_BINS + ((key[r] >> (a.shift + EMB_DIGIT)) & (EMB_BINS - 1))], 1u);
   }
 }
 
@@ -342,7 +338,7 @@ struct EmbedSum {
   unsigned* present;           // NULL: no row has tokens
   int64_t n, vocab, tiles, table_stride, row_stride;
   int64_t join_blocks;         // second launch: workgroups that join runs; the others clear rows
-  int width, tpr, accumulate, past;
+  int width, tpr, run, accumulate, past;
   float scale;
 };
 
@@ -371,7 +367,7 @@ __global__ __launch_bounds__(THREADS) void embed_sum_kernel(EmbedSum a) {
   const int64_t tile = (int64_t)blockIdx.x * (THREADS / a.tpr) + sub;
   const int c = ((threadIdx.x & (a.tpr - 1)) + blockIdx.y * a.tpr) * VE;
   if (tile >= a.tiles || c >= a.width) return;
-  const int64_t s0 = tile * EMB_RUN, s1 = s0 + EMB_RUN < a.n ? s0 + EMB_RUN : a.n;
+  const int64_t s0 = tile * a.run, s1 = s0 + a.run < a.n ? s0 + a.run : a.n;
   const int32_t prev = s0 > 0 ? a.key[s0 - 1] : -1, next = s1 < a.n ? a.key[s1] : -1;
   int32_t cur = a.key[s0];
   float acc[VE];
@@ -428,14 +424,14 @@ __global__ __launch_bounds__(THREADS) void embed_join_kernel(EmbedSum a) {
     const int64_t tile = blockIdx.x / slabs;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int c = ((int)(blockIdx.x - tile * slabs) * 64 + lane) * VE;
-    const int64_t s0 = tile * EMB_RUN, s1 = s0 + EMB_RUN;
+    const int64_t s0 = tile * a.run, s1 = s0 + a.run;
     const int32_t cur = a.key[s1];
     if (cur >= a.vocab || a.key[s1 - 1] != cur || (s0 > 0 && a.key[s0 - 1] == cur)) return;
     // the run's last tile: the last one whose first key is this token
     int64_t lo = tile + 1, hi = a.tiles - 1;
     while (lo < hi) {
       const int64_t mid = (lo + hi + 1) >> 1;
-      if (a.key[mid * EMB_RUN] == cur) lo = mid;
+      if (a.key[mid * a.run] == cur) lo = mid;
       else hi = mid - 1;
     }
     const bool on = c < a.width;
@@ -471,12 +467,13 @@ __global__ __launch_bounds__(THREADS) void embed_join_kernel(EmbedSum a) {
   }
   const int64_t word = blockIdx.x - a.join_blocks;
   const unsigned has = a.present != nullptr ? a.present[word] : 0;
-  const float z[VE] = {};
+  constexpr int ZE = VE == 1 ? 1 : 4;              // a 16-byte piece a thread
+  const float z[ZE] = {};
   const int rows = THREADS / a.tpr, lane = threadIdx.x & (a.tpr - 1);
   for (int r = threadIdx.x / a.tpr; r < 32; r += rows) {
     const int64_t v = word * 32 + r;
     if (v >= a.vocab || (has >> r & 1)) continue;
-    for (int c = lane * VE; c < a.width; c += a.tpr * VE) store_ve<float, VE>(a.dtable, v * a.table_stride + c, z, a.past);
+    for (int c = lane * ZE; c < a.width; c += a.tpr * ZE) store_ve<float, ZE>(a.dtable, v * a.table_stride + c, z, a.past);
   }
 }
 
@@ -546,11 +543,11 @@ int launch_embed_bwd(const pnn_embed_desc& d, const void* dout, const void* toke
       a.pos_in = (const int32_t*)(base + w.pos[1 - out]);
       a.key_out = (int32_t*)(base + w.key[out]);
       a.pos_out = (int32_t*)(base + w.pos[out]);
-      a.hist = (unsigned*)(base + w.hist) + p * w.blocks * EMB_BINS;
-      a.hist_next = p + 1 < w.passes ? a.hist + w.blocks * EMB_BINS : nullptr;
+      a.hist = (unsigned*)(base + w.hist);
       a.total = w.blocks > EMB_DIRECT ? (unsigned*)(base + w.total) : nullptr;
       a.shift = p * EMB_DIGIT;
-      if (p == 0) hipLaunchKernelGGL(embed_hist_kernel, dim3((unsigned)(clear > w.blocks ? clear : w.blocks)), block, 0, s, a);
+      if (p == 0) hipLaunchKernelGGL(embed_hist_kernel<true>, dim3((unsigned)(clear > w.blocks ? clear : w.blocks)), block, 0, s, a);
+      else hipLaunchKernelGGL(embed_hist_kernel<false>, dim3((unsigned)w.blocks), block, 0, s, a);
       if (a.total != nullptr) hipLaunchKernelGGL(embed_offset_kernel, dim3(EMB_BINS / 8), block, 0, s, a);
       if (p == 0) hipLaunchKernelGGL(embed_scatter_kernel<true>, dim3((unsigned)w.blocks), block, 0, s, a);
       else hipLaunchKernelGGL(embed_scatter_kernel<false>, dim3((unsigned)w.blocks), block, 0, s, a);
@@ -567,6 +564,7 @@ int launch_embed_bwd(const pnn_embed_desc& d, const void* dout, const void* toke
   m.n = d.n;
   m.vocab = d.vocab;
   m.tiles = w.tiles;
+  m.run = w.run;
   m.table_stride = d.table_stride;
   m.row_stride = d.row_stride;
   m.width = (int)d.width;

@@ -17,7 +17,13 @@ constexpr int EMB_DIGIT = 9;           // bits of a radix pass
 constexpr int EMB_BINS = 1 << EMB_DIGIT;
 constexpr int EMB_ITEMS = 2048;        // tokens of a sorting workgroup
 constexpr int EMB_DIRECT = 64;         // sorting workgroups up to which each sums the others' histograms itself
-constexpr int EMB_RUN = 32;            // sorted positions of a summing tile
+// Sorted positions of a summing tile: 32, fewer while the tiles (of up to 256 pieces of 8 columns) are under 1024
+// workgroups.
+inline int embed_run(int64_t n, int64_t width) {
+  int run = 32;
+  while (run > 8 && cdiv64(n, run) * cdiv64(width, 2048) < 1024) run /= 2;
+  return run;
+}
 // tokens outside the table sort as key = vocab, behind all others
 inline int embed_passes(int64_t vocab) {
   int bits = 0;
@@ -25,17 +31,18 @@ inline int embed_passes(int64_t vocab) {
   return (bits + EMB_DIGIT - 1) / EMB_DIGIT;
 }
 // Workspace of the gradient: keys and positions twice (the radix passes go from one to the other),
-// a histogram [workgroup][bin] for every pass and the sums over its workgroups, a bit for every table row, and the partial rows [tile][2][width] of runs that
+// a pass's histogram [workgroup][bin] and its sums over the workgroups, a bit for every table row, and the partial rows [tile][2][width] of runs that
 // cross tiles.
 struct EmbedWs {
   int64_t key[2], pos[2], hist, total, present, part, bytes;
   int64_t blocks, tiles, words;
-  int passes;
+  int passes, run;
 };
 inline EmbedWs embed_ws(const pnn_embed_desc& d) {
   EmbedWs w;
   w.blocks = cdiv64(d.n, EMB_ITEMS);
-  w.tiles = cdiv64(d.n, EMB_RUN);
+  w.run = embed_run(d.n, d.width);
+  w.tiles = cdiv64(d.n, w.run);
   w.words = cdiv64(d.vocab, 32);
   w.passes = embed_passes(d.vocab);
   int64_t o = 0;
@@ -46,7 +53,7 @@ inline EmbedWs embed_ws(const pnn_embed_desc& d) {
     o += round256(d.n * 4);
   }
   w.hist = o;
-  o += round256(w.passes * w.blocks * EMB_BINS * 4);
+  o += round256(w.blocks * EMB_BINS * 4);
   w.total = o;
   o += EMB_BINS * 4;
   w.present = o;
