@@ -10,10 +10,12 @@
 // right with the same A, and the states inside a tile are formed again from the state kept by the
 // forward (every SCAN_CHUNK steps).
 //
-// Few channels do not fill the device with workgroups: the sequence is then split into ranges of
-// tiles (scan_ranges), whose (A, B) a first launch sums up; each range's workgroup composes those of
-// the ranges before (backward: behind) it, in order.  That launch reads x and gate (backward: gate
-// and dh) a second time.
+// Few channels do not fill the device with workgroups: a sequence's tiles are then dealt to several
+// (scan_dealt), in order, by a ticket counter.  A workgroup publishes its tile's (A, B) as soon as the
+// tile has been loaded, and takes the state the tile starts from by applying the (A, B) of the tiles
+// since its own last one, in order.  So every element is still loaded once, and the bits do not depend
+// on which workgroup had which tile.  Nobody waits for a later ticket: the holder of the smallest
+// unpublished one waits for nothing, hence every wait ends, however few workgroups run at a time.
 #include "device_common.h"
 #include "seq_device.h"
 #include "seq_internal.h"
@@ -25,12 +27,14 @@ namespace {
 constexpr int FS = SCAN_FS, BS = SCAN_BS;
 
 struct Dims {
-  int length, channels, groups, chunks;
+  int length, channels, groups, chunks, tiles;
+  int dealt;                // workgroups a sequence's tiles are dealt to
   int past;                 // results larger than the L2 caches (store_to)
-  int ranges, range_tiles;  // ranges of the sequence and their tiles
+  int64_t chains;           // batch x groups
   pnn_seq_stride x, gate, h, dh, dx, dgate;
-  float *first;             // [batch][channels]: the state before the first (backward: gradient after the last) step
-  float2 *sum;              // [batch][ranges][channels]: (A, B) of a range
+  unsigned* tickets;        // [chains]: the next tile
+  float* first;             // [batch][channels]: the state before the first (backward: gradient after the last) step
+  float2* sum;              // [chains][tiles][64 VEC]: (A, B) of a tile, READY set in A once published
 };
 
 // f = sigmoid(g) and keep = 1 - f = exp(-g) f, each to about an ulp (keep is not formed by subtraction).
@@ -107,26 +111,105 @@ __device__ __forceinline__ int length_of(const int32_t* lengths, int64_t b, int 
   return n < 0 ? 0 : n > length ? length : n;
 }
 
-// The workgroup's place: channel group fastest, then range, then sequence
+// The workgroup's sequence and channels: neighbouring workgroups have neighbouring channels of the same tiles
 struct Place {
-  int group, range, wave, lane, c, cc;
-  int64_t b;
+  int wave, lane, c, cc;
+  int64_t chain, b;
   bool on;
 };
 template <int VEC>
-__device__ __forceinline__ Place place(const Dims& d, int ranges) {
+__device__ __forceinline__ Place place(const Dims& d) {
   Place p;
-  const int64_t i = blockIdx.x;
-  p.group = (int)(i % d.groups);
-  p.range = (int)(i / d.groups % ranges);
-  p.b = i / ((int64_t)d.groups * ranges);
+  p.chain = blockIdx.x % d.chains;
+  p.b = p.chain / d.groups;
   p.lane = threadIdx.x & 63;
   p.wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  p.c = (p.group * 64 + p.lane) * VEC;
+  p.c = ((int)(p.chain - p.b * d.groups) * 64 + p.lane) * VEC;
   p.on = p.c < d.channels;
   p.cc = p.on ? p.c : d.channels - VEC;    // lanes past the end load what the last one does
   return p;
 }
+
+// ---- tiles dealt to several workgroups ---------------------------------------------------------
+
+// A is never negative, so its sign bit tells a published pair from the zeros written ahead of the launch; the pair is
+// one 8-byte word, stored and loaded whole at the device-wide level.
+constexpr unsigned long long READY = 0x80000000ull;
+constexpr int LOOK = 32;                   // tiles looked back at together
+// Polls after which a thread gives up for good (seconds; a wait takes microseconds): what it would have waited for
+// becomes NaN instead of the device hanging.
+constexpr int MAX_POLLS = 1 << 22;
+
+__device__ __forceinline__ void publish(float2* at, float A, float B) {
+  const unsigned long long v = (unsigned long long)__float_as_uint(B) << 32 | __float_as_uint(A) | READY;
+  __hip_atomic_store((unsigned long long*)at, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// known (of wave 0) from the state in front of tile k0 to that in front of tile k1, through the tiles' published pairs.
+// Called by the whole workgroup; look: LOOK x 64 VEC pairs of LDS, free at the call.
+template <int VEC, int NW>
+__device__ __forceinline__ void look_back(const Dims& d, const Place& p, int k0, int k1, float (&known)[VEC], float2* look,
+                                          bool& gave_up) {
+  constexpr int CH = 64 * VEC;
+  for (int j0 = k0; j0 < k1; j0 += LOOK) {
+    const int m = k1 - j0 < LOOK ? k1 - j0 : LOOK;
+    const unsigned long long* src = (const unsigned long long*)(d.sum + (p.chain * d.tiles + j0) * CH);
+    for (int i = threadIdx.x; i < m * CH; i += 64 * NW) {
+      unsigned long long v = __hip_atomic_load(src + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      for (int n = 0; !(v & READY) && !gave_up; ++n) {
+        __builtin_amdgcn_s_sleep(1);
+        v = __hip_atomic_load(src + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        gave_up = n >= MAX_POLLS;
+      }
+      const float A = v & READY ? __uint_as_float((unsigned)v & 0x7fffffffu) : __builtin_nanf("");
+      look[i] = make_float2(A, __uint_as_float((unsigned)(v >> 32)));
+    }
+    __syncthreads();
+    if (p.wave == 0)
+#pragma unroll 4
+      for (int j = 0; j < m; ++j)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          const float2 n = look[(j * 64 + p.lane) * VEC + e];
+          known[e] = fmaf(n.x, known[e], n.y);
+        }
+    if (j0 + LOOK < k1) __syncthreads();   // before `look` is filled again
+  }
+}
+
+// Before a launch with dealt tiles: no ticket taken, nothing published, the first states (dh0 may replace dhT, hT h0).
+__global__ __launch_bounds__(256) void scan_begin_kernel(Dims d, const float* from, int64_t states, int64_t pairs) {
+  const int64_t i0 = (int64_t)blockIdx.x * 256 + threadIdx.x, step = (int64_t)gridDim.x * 256;
+  for (int64_t i = i0; i < pairs; i += step) d.sum[i] = make_float2(0.0f, 0.0f);
+  for (int64_t i = i0; i < states; i += step) d.first[i] = from != nullptr ? from[i] : 0.0f;
+  for (int64_t i = i0; i < d.chains; i += step) d.tickets[i] = 0;
+}
+
+// The tiles of a workgroup, in order: all of them, or by ticket.  `next` is taken one tile ahead, so that its loads can
+// be in flight while `cur` is worked on.
+template <bool DEALT>
+struct Tiles {
+  int cur, next;
+  unsigned* ticket;
+  __device__ __forceinline__ Tiles(const Dims& d, const Place& p, int* lds) {
+    ticket = d.tickets + p.chain;
+    cur = 0;
+    next = 1;
+    if constexpr (DEALT) {
+      if (threadIdx.x == 0) {
+        lds[0] = (int)__hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        lds[1] = (int)__hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      }
+      __syncthreads();
+      cur = __builtin_amdgcn_readfirstlane(lds[0]);
+      next = __builtin_amdgcn_readfirstlane(lds[1]);
+    }
+  }
+  // thread 0: the ticket after next
+  __device__ __forceinline__ int request() {
+    return DEALT && threadIdx.x == 0 ? (int)__hip_atomic_fetch_add(ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0;
+  }
+};
 
 // f and b = (1 - f) x of the steps; identity from `end` on
 template <typename T, int VEC, int S>
@@ -159,100 +242,39 @@ __device__ __forceinline__ void gates(const typename Raw<T, VEC>::U (&rx)[S], co
 
 // ---- forward --------------------------------------------------------------------------------
 
-// (A, B) of every range but the last; each wave takes a contiguous part of the range
-template <typename T, int VEC, int NW>
-__global__ __launch_bounds__(64 * NW) void scan_fwd_sum_kernel(Dims d, ScanArgs a) {
-  typedef typename Raw<T, VEC>::U U;
-  __shared__ float2 part[NW][64][VEC];
-  const Place p = place<VEC>(d, d.ranges - 1);
-  const int len = length_of(a.lengths, p.b, d.length);
-  const int t0 = p.range * d.range_tiles * (NW * FS) + p.wave * d.range_tiles * FS;
-  const int t1 = t0 + d.range_tiles * FS;
-  float A[VEC], B[VEC];
-#pragma unroll
-  for (int e = 0; e < VEC; ++e) {
-    A[e] = 1.0f;
-    B[e] = 0.0f;
-  }
-  // two register sets of 8 steps: one is loaded while the other is summed
-  U rx[2][8], rg[2][8];
-  auto load = [&](int k, int t) {
-    load_steps<T, VEC, 8>(rx[k], a.x, d.x, p.b, t, len, p.cc, U(0));
-    load_steps<T, VEC, 8>(rg[k], a.gate, d.gate, p.b, t, len, p.cc, U(0));
-  };
-  auto add = [&](int k, int t) {
-#pragma unroll
-    for (int s = 0; s < 8; ++s) {
-      float x[VEC], g[VEC];
-      Raw<T, VEC>::get(rx[k][s], x);
-      Raw<T, VEC>::get(rg[k][s], g);
-      if (t + s < len)
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-          float f, keep;
-          gate_of<T>(g[e], f, keep);
-          A[e] *= f;
-          B[e] = fmaf(f, B[e], keep * x[e]);
-        }
-    }
-  };
-  static_assert(FS == 16, "two sets a tile");
-  load(0, t0);
-  for (int t = t0; t < t1 && t < len; t += FS) {
-    load(1, t + 8);
-    add(0, t);
-    if (t + FS < t1) load(0, t + FS);
-    add(1, t + 8);
-  }
-#pragma unroll
-  for (int e = 0; e < VEC; ++e) part[p.wave][p.lane][e] = make_float2(A[e], B[e]);
-  __syncthreads();
-  if (p.wave != 0 || !p.on) return;
-#pragma unroll
-  for (int e = 0; e < VEC; ++e) {
-    for (int w = 1; w < NW; ++w) {
-      const float2 n = part[w][p.lane][e];
-      A[e] *= n.x;
-      B[e] = fmaf(n.x, B[e], n.y);
-    }
-    d.sum[(p.b * d.ranges + p.range) * d.channels + p.c + e] = make_float2(A[e], B[e]);
-    if (p.range == 0) d.first[p.b * d.channels + p.c + e] = a.h0 != nullptr ? a.h0[p.b * d.channels + p.c + e] : 0.0f;
-  }
-}
-
-template <typename T, int VEC, int NW>
+template <typename T, int VEC, int NW, bool DEALT>
 __global__ __launch_bounds__(64 * NW) void scan_fwd_kernel(Dims d, ScanArgs a) {
   typedef typename Raw<T, VEC>::U U;
   constexpr int L = NW * FS;
   __shared__ float2 part[2][NW][64][VEC];
-  const Place p = place<VEC>(d, d.ranges);
-  const int len = length_of(a.lengths, p.b, d.length);
-  const int r0 = p.range * d.range_tiles * L;
-  const int r1 = r0 + d.range_tiles * L < d.length ? r0 + d.range_tiles * L : d.length;
+  __shared__ float2 look[DEALT ? LOOK * 64 * VEC : 1];
+  __shared__ float start[64][VEC];
+  __shared__ int ticket[2];
+  const Place p = place<VEC>(d);
+  const int len = length_of(a.lengths, p.b, d.length), end = d.length;
+  Tiles<DEALT> tiles(d, p, ticket);
   U rx[FS], rg[FS];
-  load_steps<T, VEC, FS>(rx, a.x, d.x, p.b, r0 + p.wave * FS, len, p.cc, U(0));
-  load_steps<T, VEC, FS>(rg, a.gate, d.gate, p.b, r0 + p.wave * FS, len, p.cc, U(0));
+  auto load = [&](int k) {
+    load_steps<T, VEC, FS>(rx, a.x, d.x, p.b, k * L + p.wave * FS, len, p.cc, U(0));
+    load_steps<T, VEC, FS>(rg, a.gate, d.gate, p.b, k * L + p.wave * FS, len, p.cc, U(0));
+  };
+  if (tiles.cur < d.tiles) load(tiles.cur);
+  // the state in front of the tile at hand; DEALT: of wave 0, in front of tile `known`
   float carry[VEC];
-  const float* first = d.ranges > 1 ? d.first : a.h0;
+  int known = 0;
+  bool gave_up = false;
+  const float* first = DEALT ? d.first : a.h0;
 #pragma unroll
   for (int e = 0; e < VEC; ++e) carry[e] = first != nullptr ? first[p.b * d.channels + p.cc + e] : 0.0f;
-#pragma unroll 8
-  for (int r = 0; r < p.range; ++r)
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) {
-      const float2 n = d.sum[(p.b * d.ranges + r) * d.channels + p.cc + e];
-      carry[e] = fmaf(n.x, carry[e], n.y);
-    }
   T* const hp = (T*)a.h + p.b * d.h.batch;
+  bool last = d.tiles == 0;
   int buf = 0;
-  for (int tile = r0; tile < r1; tile += L, buf ^= 1) {
-    const int t = tile + p.wave * FS;
+  while (tiles.cur < d.tiles) {
+    const int k = tiles.cur, t = k * L + p.wave * FS;
+    const int after = tiles.request();
     float f[FS][VEC], b[FS][VEC], A[VEC], B[VEC], h[VEC];
     gates<T, VEC, FS>(rx, rg, t, len, f, b);
-    if (tile + L < r1) {
-      load_steps<T, VEC, FS>(rx, a.x, d.x, p.b, t + L, len, p.cc, U(0));
-      load_steps<T, VEC, FS>(rg, a.gate, d.gate, p.b, t + L, len, p.cc, U(0));
-    }
+    if (tiles.next < d.tiles) load(tiles.next);
 #pragma unroll
     for (int e = 0; e < VEC; ++e) {
       A[e] = 1.0f;
@@ -268,6 +290,47 @@ __global__ __launch_bounds__(64 * NW) void scan_fwd_kernel(Dims d, ScanArgs a) {
 #pragma unroll
       for (int e = 0; e < VEC; ++e) part[buf][p.wave][p.lane][e] = make_float2(A[e], B[e]);
       __syncthreads();
+    }
+    if constexpr (DEALT) {
+      // wave 0: the tile's pair, published; the state in front of the tile, then behind it (by the pair, so that the
+      // bits are those another workgroup would get)
+      if (p.wave == 0) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          A[e] = 1.0f;
+          B[e] = 0.0f;
+        }
+#pragma unroll 4
+        for (int w = 0; w < NW; ++w)
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) {
+            const float2 n = part[buf][w][p.lane][e];
+            A[e] *= n.x;
+            B[e] = fmaf(n.x, B[e], n.y);
+          }
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) publish(d.sum + ((p.chain * d.tiles + k) * 64 + p.lane) * VEC + e, A[e], B[e]);
+      }
+      look_back<VEC, NW>(d, p, known, k, carry, look, gave_up);
+      if (p.wave == 0)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          start[p.lane][e] = carry[e];
+          carry[e] = fmaf(A[e], carry[e], B[e]);
+        }
+      known = k + 1;
+      if (threadIdx.x == 0) ticket[0] = after;
+      __syncthreads();
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) h[e] = start[p.lane][e];
+#pragma unroll 4
+      for (int w = 0; w < p.wave; ++w)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          const float2 n = part[buf][w][p.lane][e];
+          h[e] = fmaf(n.x, h[e], n.y);
+        }
+    } else if constexpr (NW > 1) {
 #pragma unroll 4
       for (int w = 0; w < NW; ++w)
 #pragma unroll
@@ -299,114 +362,59 @@ __global__ __launch_bounds__(64 * NW) void scan_fwd_kernel(Dims d, ScanArgs a) {
           h[e] = fmaf(f[s][e], h[e], b[s][e]);
           o[e] = t + s < len ? h[e] : 0.0f;
         }
-        if (p.on && t + s < r1) *at<U>(hp + (int64_t)(t + s) * d.h.step, p.c * sizeof(T)) = Raw<T, VEC>::put(o);
+        if (p.on && t + s < end) *at<U>(hp + (int64_t)(t + s) * d.h.step, p.c * sizeof(T)) = Raw<T, VEC>::put(o);
       }
     }
+    last = k == d.tiles - 1;
+    tiles.cur = tiles.next;
+    tiles.next = DEALT ? __builtin_amdgcn_readfirstlane(ticket[0]) : tiles.next + 1;
+    buf ^= 1;
   }
-  if (a.hT != nullptr && p.range == d.ranges - 1 && p.wave == 0 && p.on)
+  if (a.hT != nullptr && last && p.wave == 0 && p.on)
 #pragma unroll
     for (int e = 0; e < VEC; ++e) a.hT[p.b * d.channels + p.c + e] = carry[e];
 }
 
 // ---- backward -------------------------------------------------------------------------------
 
-// (A, B) of every range but the first, for the chain from the right: c -> A c + B
-template <typename T, int VEC, int NW>
-__global__ __launch_bounds__(64 * NW) void scan_bwd_sum_kernel(Dims d, ScanArgs a) {
-  typedef typename Raw<T, VEC>::U U;
-  __shared__ float2 part[NW][64][VEC];
-  const Place p = place<VEC>(d, d.ranges - 1);
-  const int range = p.range + 1;
-  const int len = length_of(a.lengths, p.b, d.length);
-  const int t0 = range * d.range_tiles * (NW * BS) + p.wave * d.range_tiles * BS;
-  const int t1 = t0 + d.range_tiles * BS;
-  float A[VEC], B[VEC];
-#pragma unroll
-  for (int e = 0; e < VEC; ++e) {
-    A[e] = 1.0f;
-    B[e] = 0.0f;
-  }
-  U rg[BS], rd[BS];
-  load_steps<T, VEC, BS>(rg, a.gate, d.gate, p.b, t1 - BS, len, p.cc, U(0));
-  load_steps<T, VEC, BS>(rd, a.dh, d.dh, p.b, t1 - BS, len, p.cc, U(0));
-  for (int t = t1 - BS; t >= t0; t -= BS) {
-    float f[BS][VEC], g[BS][VEC];
-#pragma unroll
-    for (int s = 0; s < BS; ++s) {
-      float v[VEC], keep;
-      Raw<T, VEC>::get(rg[s], v);
-      Raw<T, VEC>::get(rd[s], g[s]);
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) gate_of<T>(v[e], f[s][e], keep);
-    }
-    if (t > t0) {
-      load_steps<T, VEC, BS>(rg, a.gate, d.gate, p.b, t - BS, len, p.cc, U(0));
-      load_steps<T, VEC, BS>(rd, a.dh, d.dh, p.b, t - BS, len, p.cc, U(0));
-    }
-#pragma unroll
-    for (int s = BS - 1; s >= 0; --s)
-      if (t + s < len)
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) {
-          A[e] *= f[s][e];
-          B[e] = f[s][e] * (g[s][e] + B[e]);
-        }
-  }
-#pragma unroll
-  for (int e = 0; e < VEC; ++e) part[p.wave][p.lane][e] = make_float2(A[e], B[e]);
-  __syncthreads();
-  if (p.wave != NW - 1 || !p.on) return;
-#pragma unroll
-  for (int e = 0; e < VEC; ++e) {
-    for (int w = NW - 2; w >= 0; --w) {
-      const float2 n = part[w][p.lane][e];
-      A[e] *= n.x;
-      B[e] = fmaf(n.x, B[e], n.y);
-    }
-    d.sum[(p.b * d.ranges + range) * d.channels + p.c + e] = make_float2(A[e], B[e]);
-    if (range == d.ranges - 1)
-      d.first[p.b * d.channels + p.c + e] = a.dhT != nullptr ? a.dhT[p.b * d.channels + p.c + e] : 0.0f;
-  }
-}
-
-template <typename T, int VEC, int NW>
+// Tile k of the chain is the k-th from the sequence's end.
+template <typename T, int VEC, int NW, bool DEALT>
 __global__ __launch_bounds__(64 * NW) void scan_bwd_kernel(Dims d, ScanArgs a) {
   typedef typename Raw<T, VEC>::U U;
   constexpr int L = NW * BS;
   static_assert(NW < SCAN_NW || L == SCAN_CHUNK, "tiles start at kept states (fewer waves: one tile)");
   __shared__ float2 part[2][NW][64][VEC];
   __shared__ float back[2][NW][64][VEC];
-  const Place p = place<VEC>(d, d.ranges);
-  const int len = length_of(a.lengths, p.b, d.length);
-  const int r0 = p.range * d.range_tiles * L;
-  const int r1 = r0 + d.range_tiles * L < d.length ? r0 + d.range_tiles * L : d.length;
-  const int last = r1 > r0 ? r0 + (r1 - r0 - 1) / L * L : r0 - L;   // no step: no tile
+  __shared__ float2 look[DEALT ? LOOK * 64 * VEC : 1];
+  __shared__ float start[64][VEC];
+  __shared__ int ticket[2];
+  const Place p = place<VEC>(d);
+  const int len = length_of(a.lengths, p.b, d.length), end = d.length;
+  Tiles<DEALT> tiles(d, p, ticket);
   U rx[BS], rg[BS], rd[BS];
   float state[VEC], carry[VEC];
-  auto load = [&](int tile) {
-    const int t = tile + p.wave * BS;
+  auto load = [&](int k) {
+    const int tile = d.tiles - 1 - k, t = tile * L + p.wave * BS;
     load_steps<T, VEC, BS>(rx, a.x, d.x, p.b, t, len, p.cc, U(0));
     load_steps<T, VEC, BS>(rg, a.gate, d.gate, p.b, t, len, p.cc, U(0));
     load_steps<T, VEC, BS>(rd, a.dh, d.dh, p.b, t, len, p.cc, U(0));
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) state[e] = a.states[(p.b * d.chunks + tile / SCAN_CHUNK) * d.channels + p.cc + e];
+    for (int e = 0; e < VEC; ++e) state[e] = a.states[(p.b * d.chunks + tile) * d.channels + p.cc + e];
   };
-  if (last >= r0) load(last);
-  const float* first = d.ranges > 1 ? d.first : a.dhT;
+  if (tiles.cur < d.tiles) load(tiles.cur);
+  // the gradient from behind the tile at hand; DEALT: of wave 0, from behind tile `known`
+  int known = 0;
+  bool gave_up = false;
+  const float* first = DEALT ? d.first : a.dhT;
 #pragma unroll
   for (int e = 0; e < VEC; ++e) carry[e] = first != nullptr ? first[p.b * d.channels + p.cc + e] : 0.0f;
-#pragma unroll 8
-  for (int r = d.ranges - 1; r > p.range; --r)
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) {
-      const float2 n = d.sum[(p.b * d.ranges + r) * d.channels + p.cc + e];
-      carry[e] = fmaf(n.x, carry[e], n.y);
-    }
   T* const xp = (T*)a.dx + p.b * d.dx.batch;
   T* const gp = (T*)a.dgate + p.b * d.dgate.batch;
+  bool last = d.tiles == 0;
   int buf = 0;
-  for (int tile = last; tile >= r0; tile -= L, buf ^= 1) {
-    const int t = tile + p.wave * BS;
+  while (tiles.cur < d.tiles) {
+    const int k = tiles.cur, t = (d.tiles - 1 - k) * L + p.wave * BS;
+    const int after = tiles.request();
     float f[BS][VEC], keep[BS][VEC], x[BS][VEC], g[BS][VEC], h[VEC], c[VEC];
 #pragma unroll
     for (int s = 0; s < BS; ++s) {
@@ -429,7 +437,7 @@ __global__ __launch_bounds__(64 * NW) void scan_bwd_kernel(Dims d, ScanArgs a) {
     }
 #pragma unroll
     for (int e = 0; e < VEC; ++e) h[e] = state[e];
-    if (tile > r0) load(tile - L);
+    if (tiles.next < d.tiles) load(tiles.next);
     float A[VEC], B[VEC], C[VEC];
 #pragma unroll
     for (int e = 0; e < VEC; ++e) {
@@ -450,17 +458,50 @@ __global__ __launch_bounds__(64 * NW) void scan_bwd_kernel(Dims d, ScanArgs a) {
         back[buf][p.wave][p.lane][e] = C[e];
       }
       __syncthreads();
-      float first_h[VEC];
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) first_h[e] = h[e];
+      // h: from the kept state through the waves before this one
 #pragma unroll 4
-      for (int w = 0; w < NW; ++w)
+      for (int w = 0; w < p.wave; ++w)
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
-          if (w == p.wave) h[e] = first_h[e];
           const float2 n = part[buf][w][p.lane][e];
-          first_h[e] = fmaf(n.x, first_h[e], n.y);
+          h[e] = fmaf(n.x, h[e], n.y);
         }
+    }
+    if constexpr (DEALT) {
+      if (p.wave == 0) {       // as in the forward, from the right
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          A[e] = 1.0f;
+          C[e] = 0.0f;
+        }
+#pragma unroll 4
+        for (int w = NW - 1; w >= 0; --w)
+#pragma unroll
+          for (int e = 0; e < VEC; ++e) {
+            const float n = part[buf][w][p.lane][e].x;
+            A[e] *= n;
+            C[e] = fmaf(n, C[e], back[buf][w][p.lane][e]);
+          }
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) publish(d.sum + ((p.chain * d.tiles + k) * 64 + p.lane) * VEC + e, A[e], C[e]);
+      }
+      look_back<VEC, NW>(d, p, known, k, carry, look, gave_up);
+      if (p.wave == 0)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          start[p.lane][e] = carry[e];
+          carry[e] = fmaf(A[e], carry[e], C[e]);
+        }
+      known = k + 1;
+      if (threadIdx.x == 0) ticket[0] = after;
+      __syncthreads();
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) c[e] = start[p.lane][e];
+#pragma unroll 4
+      for (int w = NW - 1; w > p.wave; --w)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) c[e] = fmaf(part[buf][w][p.lane][e].x, c[e], back[buf][w][p.lane][e]);
+    } else if constexpr (NW > 1) {
 #pragma unroll 4
       for (int w = NW - 1; w >= 0; --w)
 #pragma unroll
@@ -490,13 +531,17 @@ __global__ __launch_bounds__(64 * NW) void scan_bwd_kernel(Dims d, ScanArgs a) {
         og[e] = ox[e] * f[s][e] * x[s][e];
         c[e] = f[s][e] * G;
       }
-      if (p.on && t + s < r1) {
+      if (p.on && t + s < end) {
         store_to(at<U>(xp + (int64_t)(t + s) * d.dx.step, p.c * sizeof(T)), Raw<T, VEC>::put(ox), d.past);
         store_to(at<U>(gp + (int64_t)(t + s) * d.dgate.step, p.c * sizeof(T)), Raw<T, VEC>::put(og), d.past);
       }
     }
+    last = k == d.tiles - 1;
+    tiles.cur = tiles.next;
+    tiles.next = DEALT ? __builtin_amdgcn_readfirstlane(ticket[0]) : tiles.next + 1;
+    buf ^= 1;
   }
-  if (a.dh0 != nullptr && p.range == 0 && p.wave == 0 && p.on)
+  if (a.dh0 != nullptr && last && p.wave == 0 && p.on)
 #pragma unroll
     for (int e = 0; e < VEC; ++e) a.dh0[p.b * d.channels + p.c + e] = carry[e];
 }
@@ -510,12 +555,9 @@ Dims dims(const pnn_scan_desc& d, const ScanArgs& a, int vec, int tile) {
   m.channels = (int)d.channels;
   m.groups = (int)cdiv64(d.channels, 64 * vec);
   m.chunks = (int)scan_chunks(d);
-  const int64_t tiles = cdiv64(d.length, tile);
-  const int64_t ranges = scan_ranges(d.batch * m.groups, tiles);
-  m.range_tiles = (int)cdiv64(tiles, ranges);
-  if (m.range_tiles < 1) m.range_tiles = 1;
-  m.ranges = (int)cdiv64(tiles, m.range_tiles);
-  if (m.ranges < 1) m.ranges = 1;
+  m.tiles = (int)cdiv64(d.length, tile);
+  m.chains = d.batch * m.groups;
+  m.dealt = scan_dealt(m.chains, m.tiles);
   m.past = d.batch * d.length * d.channels * (d.dtype == PNN_F32 ? 4 : 2) > L2_BYTES;
   m.x = d.x;
   m.gate = d.gate;
@@ -523,25 +565,36 @@ Dims dims(const pnn_scan_desc& d, const ScanArgs& a, int vec, int tile) {
   m.dh = d.dh;
   m.dx = d.dx;
   m.dgate = d.dgate;
-  m.first = (float*)a.ws;
-  m.sum = (float2*)((char*)a.ws + round256(d.batch * d.channels * 4));
+  const ScanWs w = scan_ws(d.batch * d.channels, m.chains, m.tiles, vec);
+  m.tickets = (unsigned*)((char*)a.ws + w.tickets);
+  m.first = (float*)((char*)a.ws + w.first);
+  m.sum = (float2*)((char*)a.ws + w.sum);
   return m;
+}
+
+void begin(const Dims& m, const float* from, int64_t states, int vec, hipStream_t s) {
+  const int64_t pairs = m.chains * m.tiles * 64 * vec, n = pairs > states ? pairs : states;
+  const int64_t grid = cdiv64(n, 1024) < 4096 ? cdiv64(n, 1024) : 4096;
+  hipLaunchKernelGGL(scan_begin_kernel, dim3((unsigned)grid), dim3(256), 0, s, m, from, states, pairs);
 }
 
 }  // namespace
 
 int launch_scan_fwd(const pnn_scan_desc& d, const ScanArgs& a, hipStream_t s) {
   const int nw = d.length <= FS ? 1 : d.length <= 4 * FS ? 4 : 16;
-  const bool pair = d.dtype == PNN_BF16 && d.channels % 2 == 0 && al4(a.x) && al4(a.gate) && al4(a.h) && even(d.x) &&
+  const bool pair = d.dtype == PNN_BF16 && scan_pairs(d, false) && al4(a.x) && al4(a.gate) && al4(a.h) && even(d.x) &&
                     even(d.gate) && even(d.h);
 #define FWD(T, VEC, NW)                                                                                             \
   do {                                                                                                              \
     const Dims m = dims(d, a, VEC, NW * FS);                                                                        \
-    const int64_t n = d.batch * m.groups;                                                                           \
+    const dim3 grid((unsigned)(m.chains * m.dealt)), block(64 * NW);                                                \
     if constexpr (NW == SCAN_NW) /* fewer waves: a single tile */                                                   \
-      if (m.ranges > 1)                                                                                             \
-        hipLaunchKernelGGL((scan_fwd_sum_kernel<T, VEC, NW>), dim3((unsigned)(n * (m.ranges - 1))), dim3(64 * NW), 0, s, m, a); \
-    hipLaunchKernelGGL((scan_fwd_kernel<T, VEC, NW>), dim3((unsigned)(n * m.ranges)), dim3(64 * NW), 0, s, m, a);   \
+      if (m.dealt > 1) {                                                                                            \
+        begin(m, a.h0, d.batch * d.channels, VEC, s);                                                               \
+        hipLaunchKernelGGL((scan_fwd_kernel<T, VEC, NW, true>), grid, block, 0, s, m, a);                           \
+        break;                                                                                                      \
+      }                                                                                                             \
+    hipLaunchKernelGGL((scan_fwd_kernel<T, VEC, NW, false>), grid, block, 0, s, m, a);                              \
   } while (0)
 #define FWD_NW(T, VEC)                \
   do {                                \
@@ -559,16 +612,19 @@ int launch_scan_fwd(const pnn_scan_desc& d, const ScanArgs& a, hipStream_t s) {
 
 int launch_scan_bwd(const pnn_scan_desc& d, const ScanArgs& a, hipStream_t s) {
   const int nw = d.length <= BS ? 1 : d.length <= 4 * BS ? 4 : 16;
-  const bool pair = d.dtype == PNN_BF16 && d.channels % 2 == 0 && al4(a.x) && al4(a.gate) && al4(a.dh) && al4(a.dx) &&
+  const bool pair = d.dtype == PNN_BF16 && scan_pairs(d, true) && al4(a.x) && al4(a.gate) && al4(a.dh) && al4(a.dx) &&
                     al4(a.dgate) && even(d.x) && even(d.gate) && even(d.dh) && even(d.dx) && even(d.dgate);
 #define BWD(T, VEC, NW)                                                                                             \
   do {                                                                                                              \
     const Dims m = dims(d, a, VEC, NW * BS);                                                                        \
-    const int64_t n = d.batch * m.groups;                                                                           \
+    const dim3 grid((unsigned)(m.chains * m.dealt)), block(64 * NW);                                                \
     if constexpr (NW == SCAN_NW) /* fewer waves: a single tile */                                                   \
-      if (m.ranges > 1)                                                                                             \
-        hipLaunchKernelGGL((scan_bwd_sum_kernel<T, VEC, NW>), dim3((unsigned)(n * (m.ranges - 1))), dim3(64 * NW), 0, s, m, a); \
-    hipLaunchKernelGGL((scan_bwd_kernel<T, VEC, NW>), dim3((unsigned)(n * m.ranges)), dim3(64 * NW), 0, s, m, a);   \
+      if (m.dealt > 1) {                                                                                            \
+        begin(m, a.dhT, d.batch * d.channels, VEC, s);                                                               \
+        hipLaunchKernelGGL((scan_bwd_kernel<T, VEC, NW, true>), grid, block, 0, s, m, a);                           \
+        break;                                                                                                      \
+      }                                                                                                             \
+    hipLaunchKernelGGL((scan_bwd_kernel<T, VEC, NW, false>), grid, block, 0, s, m, a);                              \
   } while (0)
 #define BWD_NW(T, VEC)                \
   do {                                \

@@ -163,6 +163,8 @@ SCAN = [
     (1, 1025, 65, "bf16", "dense", None, True, 0),
     (2, 1537, 66, "bf16", "time", "ragged", True, 0),
     (1, 5003, 9, "f32", "dense", None, True, 0),
+    (100, 1500, 30, "bf16", "halves", "ragged", True, 0),        # several tiles for each of two workgroups
+    (40, 2311, 66, "f32", "dense", "ragged", True, 0),           # two channel groups, three workgroups each
 ]
 
 
