@@ -90,6 +90,30 @@ bool al16p(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
 // ---- sort -------------------------------------------------------------------------------------
 
+// Rows of the gradient to clear: [row0, row1), 32 to a workgroup.
+struct ClearRows {
+  float* dtable;
+  int64_t table_stride, row0, row1;
+  int width, wide, past;
+};
+// ZE elements a thread and store; `has`: bits of rows that are left as they are
+template <int ZE>
+__device__ __forceinline__ void clear_word(const ClearRows& a, int64_t row, unsigned has) {
+  const float z[ZE] = {};
+  int tpr = 1;
+  while (tpr < (int)blockDim.x && tpr * ZE < a.width) tpr *= 2;
+  const int rows = blockDim.x / tpr, lane = threadIdx.x & (tpr - 1);
+  for (int r = threadIdx.x / tpr; r < 32; r += rows) {
+    const int64_t v = row + r;
+    if (v >= a.row1 || (has >> r & 1)) continue;
+    for (int c = lane * ZE; c < a.width; c += tpr * ZE) store_ve<float, ZE>(a.dtable, v * a.table_stride + c, z, a.past);
+  }
+}
+__device__ __forceinline__ void clear_word(const ClearRows& a, int64_t word, unsigned has) {
+  if (a.wide) clear_word<4>(a, a.row0 + word * 32, has);
+  else clear_word<1>(a, a.row0 + word * 32, has);
+}
+
 struct EmbedSort {
   const void* tokens;          // first pass: keys from the tokens, positions 0, 1, ..
   const int32_t *key_in, *pos_in;
@@ -99,7 +123,17 @@ struct EmbedSort {
   unsigned* present;           // a bit for every row of the table, cleared by the first launch (embed_sum_kernel sets them)
   int64_t n, vocab, blocks, words;
   int token_bytes, shift, passes;
+  // The sort leaves the memory idle: the workgroups of its launches behind the first clear_from clear some rows of the
+  // gradient, whether or not the sums will write them.
+  int64_t clear_from;
+  ClearRows clear;
 };
+
+__device__ __forceinline__ bool clears_rows(const EmbedSort& a) {
+  if (blockIdx.x < a.clear_from) return false;
+  clear_word(a.clear, blockIdx.x - a.clear_from, 0);
+  return true;
+}
 
 // key and position of item i; past the end the last one's (not to be used)
 template <bool FIRST>
@@ -116,7 +150,7 @@ __device__ __forceinline__ void item(const EmbedSort& a, int64_t i, int32_t& key
 }
 
 __device__ __forceinline__ void clear_present(const EmbedSort& a) {
-  for (int64_t w = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; w < a.words; w += (int64_t)gridDim.x * blockDim.x)
+  for (int64_t w = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; w < a.words; w += a.clear_from * blockDim.x)
     a.present[w] = 0;
 }
 
@@ -126,6 +160,7 @@ __device__ __forceinline__ void clear_present(const EmbedSort& a) {
 template <bool FIRST>
 __global__ __launch_bounds__(THREADS) void embed_hist_kernel(EmbedSort a) {
   __shared__ unsigned cnt[EMB_BINS];
+  if (clears_rows(a)) return;
   if (FIRST) clear_present(a);
   if (blockIdx.x >= a.blocks) return;
   for (int b = threadIdx.x; b < EMB_BINS; b += THREADS) cnt[b] = 0;
@@ -236,6 +271,7 @@ __global__ __launch_bounds__(THREADS) void embed_scatter_kernel(EmbedSort a) {
   constexpr int WAVES = THREADS / 64, ROUNDS = EMB_ITEMS / THREADS;
   __shared__ unsigned base[WAVES][EMB_BINS];
   __shared__ unsigned wsum[WAVES];
+  if (clears_rows(a)) return;
   const int tid = threadIdx.x, wave = tid / 64, lane = tid & 63;
   const int64_t i0 = (int64_t)blockIdx.x * EMB_ITEMS + wave * (EMB_ITEMS / WAVES) + lane;
   int32_t key[ROUNDS], pos[ROUNDS];
@@ -282,6 +318,7 @@ __global__ __launch_bounds__(2 * THREADS) void embed_sort_kernel(EmbedSort a) {
   __shared__ unsigned base[WAVES][EMB_BINS];
   __shared__ unsigned wsum[WAVES];
   __shared__ int32_t skey[EMB_ITEMS], spos[EMB_ITEMS];
+  if (clears_rows(a)) return;
   clear_present(a);
   if (blockIdx.x > 0) return;
   const int tid = threadIdx.x, wave = tid / 64, lane = tid & 63;
@@ -340,6 +377,7 @@ struct EmbedSum {
   int64_t join_blocks;         // second launch: workgroups that join runs; the others clear rows
   int width, tpr, run, accumulate, past;
   float scale;
+  ClearRows clear;             // the rows of the second launch
 };
 
 template <int VE>
@@ -414,7 +452,7 @@ __global__ __launch_bounds__(THREADS) void embed_sum_kernel(EmbedSum a) {
 // Second launch.  Its first join_blocks workgroups join the runs over several tiles, by the tile they
 // start in: its part row 1, then the part rows 0 of the tiles up to the one the run ends in; each of
 // the JW groups of 64 threads takes every JW-th of them, the groups' sums are added in order.  The
-// others clear the rows without tokens, 32 (a word of `present`) each.
+// others clear the rows without tokens that the sort's launches left, 32 (a word of `present`) each.
 template <int VE>
 __global__ __launch_bounds__(THREADS) void embed_join_kernel(EmbedSum a) {
   constexpr int JW = THREADS / 64;
@@ -466,15 +504,7 @@ __global__ __launch_bounds__(THREADS) void embed_join_kernel(EmbedSum a) {
     return;
   }
   const int64_t word = blockIdx.x - a.join_blocks;
-  const unsigned has = a.present != nullptr ? a.present[word] : 0;
-  constexpr int ZE = VE == 1 ? 1 : 4;              // a 16-byte piece a thread
-  const float z[ZE] = {};
-  const int rows = THREADS / a.tpr, lane = threadIdx.x & (a.tpr - 1);
-  for (int r = threadIdx.x / a.tpr; r < 32; r += rows) {
-    const int64_t v = word * 32 + r;
-    if (v >= a.vocab || (has >> r & 1)) continue;
-    for (int c = lane * ZE; c < a.width; c += a.tpr * ZE) store_ve<float, ZE>(a.dtable, v * a.table_stride + c, z, a.past);
-  }
+  clear_word(a.clear, word, a.present != nullptr ? a.present[word] : 0);
 }
 
 constexpr int64_t MAX_GRID = 65536;   // workgroups of the row loops
@@ -526,31 +556,59 @@ int launch_embed_bwd(const pnn_embed_desc& d, const void* dout, const void* toke
   a.passes = w.passes;
   a.words = accumulate ? 0 : w.words;
   a.present = (unsigned*)(base + w.present);
+  const int es = d.dtype == PNN_F32 ? 4 : 2;
+  const bool wide = d.width % 8 == 0 && al16p(dtable) && al16p(dout) && d.table_stride % 4 == 0 && d.row_stride * es % 16 == 0;
+  ClearRows clear;
+  clear.dtable = dtable;
+  clear.table_stride = d.table_stride;
+  clear.width = (int)d.width;
+  clear.wide = wide;
+  clear.past = d.vocab * d.width * 4 > L2_BYTES;
+  int64_t rows = accumulate ? 0 : d.vocab;               // rows not yet taken by a launch that clears them
+  // The last rows left go to the launch to come: EMB_CLEAR bytes of them, whole words of row bits, and no more rows in
+  // all than surely have no token (8192 rows, 65536 tokens: clearing what is written again took 5 us a call) unless the
+  // tokens' rows are small (1237 tokens of 515 elements: clearing all rows 21 us, without theirs 25).  Returns the
+  // grid: the workgroups they need behind the first `blocks`.
+  const int64_t least = (d.n < d.vocab ? d.n : d.vocab) * d.width * 4 <= EMB_CLEAR / 4 ? 0 : cdiv64(d.n, 32) * 32;
+  auto take_rows = [&](int64_t blocks) {
+    const int64_t words = cdiv64(EMB_CLEAR, 32 * 4 * d.width);
+    int64_t from = rows / 32 > words ? (rows / 32 - words) * 32 : 0;
+    from = from > least ? from : least < rows ? least : rows;
+    a.clear = clear;
+    a.clear.row0 = from;
+    a.clear.row1 = rows;
+    a.clear_from = blocks;
+    const int64_t more = cdiv64(rows - from, 32);
+    rows = from;
+    return dim3((unsigned)(blocks + more));
+  };
   // launches that clear the row bits: a workgroup for at most 4096 words more
-  const int64_t clear = cdiv64(a.words, 4096) < MAX_GRID ? cdiv64(a.words, 4096) : MAX_GRID;
+  const int64_t bits = cdiv64(a.words, 4096) < MAX_GRID ? cdiv64(a.words, 4096) : MAX_GRID;
   int out = 0;
   if (d.n > 0 && w.blocks == 1) {
     a.tokens = tokens;
     a.key_out = (int32_t*)(base + w.key[0]);
     a.pos_out = (int32_t*)(base + w.pos[0]);
-    hipLaunchKernelGGL(embed_sort_kernel, dim3((unsigned)(clear > 1 ? clear : 1)), dim3(2 * THREADS), 0, s, a);
+    hipLaunchKernelGGL(embed_sort_kernel, take_rows(bits > 1 ? bits : 1), dim3(2 * THREADS), 0, s, a);
     if (const hipError_t e = hipGetLastError()) return (int)e;
   } else if (d.n > 0) {
     a.tokens = tokens;
+    a.hist = (unsigned*)(base + w.hist);
     for (int p = 0; p < w.passes; ++p) {
       out = p & 1;
       a.key_in = (const int32_t*)(base + w.key[1 - out]);
       a.pos_in = (const int32_t*)(base + w.pos[1 - out]);
       a.key_out = (int32_t*)(base + w.key[out]);
       a.pos_out = (int32_t*)(base + w.pos[out]);
-      a.hist = (unsigned*)(base + w.hist);
       a.total = w.blocks > EMB_DIRECT ? (unsigned*)(base + w.total) : nullptr;
       a.shift = p * EMB_DIGIT;
-      if (p == 0) hipLaunchKernelGGL(embed_hist_kernel<true>, dim3((unsigned)(clear > w.blocks ? clear : w.blocks)), block, 0, s, a);
-      else hipLaunchKernelGGL(embed_hist_kernel<false>, dim3((unsigned)w.blocks), block, 0, s, a);
+      const dim3 hist_grid = take_rows(p == 0 && bits > w.blocks ? bits : w.blocks);
+      if (p == 0) hipLaunchKernelGGL(embed_hist_kernel<true>, hist_grid, block, 0, s, a);
+      else hipLaunchKernelGGL(embed_hist_kernel<false>, hist_grid, block, 0, s, a);
       if (a.total != nullptr) hipLaunchKernelGGL(embed_offset_kernel, dim3(EMB_BINS / 8), block, 0, s, a);
-      if (p == 0) hipLaunchKernelGGL(embed_scatter_kernel<true>, dim3((unsigned)w.blocks), block, 0, s, a);
-      else hipLaunchKernelGGL(embed_scatter_kernel<false>, dim3((unsigned)w.blocks), block, 0, s, a);
+      const dim3 grid = take_rows(w.blocks);
+      if (p == 0) hipLaunchKernelGGL(embed_scatter_kernel<true>, grid, block, 0, s, a);
+      else hipLaunchKernelGGL(embed_scatter_kernel<false>, grid, block, 0, s, a);
       if (const hipError_t e = hipGetLastError()) return (int)e;
     }
   }
@@ -569,10 +627,11 @@ int launch_embed_bwd(const pnn_embed_desc& d, const void* dout, const void* toke
   m.row_stride = d.row_stride;
   m.width = (int)d.width;
   m.accumulate = accumulate != 0;
-  m.past = d.vocab * d.width * 4 > L2_BYTES;
+  m.past = clear.past;
+  m.clear = clear;
+  m.clear.row0 = 0;
+  m.clear.row1 = rows;
   m.scale = d.scale;
-  const int es = d.dtype == PNN_F32 ? 4 : 2;
-  const bool wide = d.width % 8 == 0 && al16p(dtable) && al16p(dout) && d.table_stride % 4 == 0 && d.row_stride * es % 16 == 0;
   const int64_t pieces = wide ? d.width / 8 : d.width;
   m.tpr = threads_per_row(pieces);
   if (d.n > 0) {
@@ -593,7 +652,7 @@ int launch_embed_bwd(const pnn_embed_desc& d, const void* dout, const void* toke
     if (const hipError_t e = hipGetLastError()) return (int)e;
   }
   m.join_blocks = (w.tiles > 1 ? w.tiles - 1 : 0) * cdiv64(d.width, 64 * (wide ? 8 : 1));
-  const int64_t blocks = m.join_blocks + (m.accumulate ? 0 : w.words);
+  const int64_t blocks = m.join_blocks + cdiv64(rows, 32);
   if (blocks == 0) return 0;
   if (wide) hipLaunchKernelGGL((embed_join_kernel<8>), dim3((unsigned)blocks), block, 0, s, m);
   else hipLaunchKernelGGL((embed_join_kernel<1>), dim3((unsigned)blocks), block, 0, s, m);

@@ -17,6 +17,7 @@ constexpr int EMB_DIGIT = 9;           // bits of a radix pass
 constexpr int EMB_BINS = 1 << EMB_DIGIT;
 constexpr int EMB_ITEMS = 2048;        // tokens of a sorting workgroup
 constexpr int EMB_DIRECT = 64;         // sorting workgroups up to which each sums the others' histograms itself
+constexpr int64_t EMB_CLEAR = 32 << 20;  // bytes of the gradient a launch of the sort clears on the side
 // Sorted positions of a summing tile: 32, fewer while the tiles (of up to 256 pieces of 8 columns) are under 1024
 // workgroups.
 inline int embed_run(int64_t n, int64_t width) {
