@@ -19,31 +19,28 @@ __device__ __forceinline__ int64_t token_at(const void* tokens, int bytes, int64
   return bytes == 8 ? ((const int64_t*)tokens)[i] : (int64_t)((const int32_t*)tokens)[i];
 }
 
-// VE consecutive elements of T as floats; VE > 1: 16-byte loads
-template <typename T, int VE>
-__device__ __forceinline__ void load_ve(const void* p, int64_t i, float* v) {
-  if constexpr (VE == 1) {
-    v[0] = St<T>::ld(p, i);
+// Elements a thread has of a row: two 16-byte pieces of float, one of bf16.  `left`: elements of the row from i on; a
+// row's last thread may have fewer than VE.
+constexpr int VE = 8;
+template <typename T>
+__device__ __forceinline__ void load_ve(const void* p, int64_t i, int left, float* v) {
+  if (left >= VE) {
+#pragma unroll
+    for (int c = 0; c < VE; c += St<T>::VE) load_piece<T>(p, i + c, v + c);
   } else {
 #pragma unroll
-    for (int c = 0; c < VE / St<T>::VE; ++c) {
-      Chunk<T> k;
-      load_chunk<T>(p, i + c * St<T>::VE, k);
-#pragma unroll
-      for (int e = 0; e < St<T>::VE; ++e) v[c * St<T>::VE + e] = k.v[e];
-    }
+    for (int e = 0; e < VE; ++e) v[e] = e < left ? St<T>::ld(p, i + e) : 0.0f;
   }
 }
-// the same to memory; `past`: see store_to
-template <typename T, int VE>
-__device__ __forceinline__ void store_ve(void* p, int64_t i, const float* v, bool past = false) {
-  if constexpr (VE == 1) {
-    if constexpr (sizeof(T) == 4) store_to((float*)p + i, v[0], past);
-    else store_to((uint16_t*)p + i, f2bf(v[0]), past);
-  } else {
-    // past the caches only whole lines: where a thread has one piece, its neighbours have the pieces around it
+template <typename T>
+__device__ __forceinline__ void store_ve(void* p, int64_t i, int left, const float* v) {
+  if (left >= VE) {
 #pragma unroll
-    for (int c = 0; c < VE; c += St<T>::VE) store_piece<T>(p, i + c, v + c, past && VE == St<T>::VE);
+    for (int c = 0; c < VE; c += St<T>::VE) store_piece<T>(p, i + c, v + c, false);
+  } else {
+#pragma unroll
+    for (int e = 0; e < VE; ++e)
+      if (e < left) St<T>::st(p, i + e, v[e]);
   }
 }
 
@@ -64,54 +61,73 @@ struct EmbedFwd {
   float scale;
 };
 
-template <typename TT, typename TO, int VE>
+// W elements of T from i on: the piece of the output's type a thread has at a time
+template <typename T, int W>
+__device__ __forceinline__ void load_w(const void* p, int64_t i, float* v) {
+  if constexpr (W >= St<T>::VE) {
+#pragma unroll
+    for (int c = 0; c < W; c += St<T>::VE) load_piece<T>(p, i + c, v + c);
+  } else {                                         // four bf16 for a piece of float
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+    typedef u32x2 Mem __attribute__((aligned(2)));
+    const u32x2 u = *(const Mem*)((const uint16_t*)p + i);
+    v[0] = __uint_as_float(u.x << 16);
+    v[1] = __uint_as_float(u.x & 0xffff0000u);
+    v[2] = __uint_as_float(u.y << 16);
+    v[3] = __uint_as_float(u.y & 0xffff0000u);
+  }
+}
+
+template <typename TT, typename TO>
 __global__ __launch_bounds__(THREADS) void embed_fwd_kernel(EmbedFwd a) {
+  constexpr int W = St<TO>::VE;
   const int rows = THREADS / a.tpr;
   const int lane = threadIdx.x & (a.tpr - 1);
   for (int64_t i = (int64_t)blockIdx.x * rows + threadIdx.x / a.tpr; i < a.n; i += (int64_t)gridDim.x * rows) {
     const int64_t t = token_at(a.tokens, a.token_bytes, i);
     const bool in = t >= 0 && t < a.vocab;
-    for (int c = lane * VE; c < a.width; c += a.tpr * VE) {
-      float v[VE];
-      if (in) {
-        load_ve<TT, VE>(a.table, t * a.table_stride + c, v);
+    const float none = t < 0 ? 0.0f : __builtin_nanf("");
+    for (int c = lane * W; c < a.width; c += a.tpr * W) {
+      const int64_t from = (in ? t : 0) * a.table_stride + c, to = i * a.row_stride + c;
+      if (c + W <= a.width) {
+        float v[W];
+        if (in) load_w<TT, W>(a.table, from, v);
 #pragma unroll
-        for (int e = 0; e < VE; ++e) v[e] *= a.scale;
+        for (int e = 0; e < W; ++e) v[e] = in ? v[e] * a.scale : none;
+        store_piece<TO>(a.out, to, v, a.past);
       } else {
-#pragma unroll
-        for (int e = 0; e < VE; ++e) v[e] = t < 0 ? 0.0f : __builtin_nanf("");
+        for (int e = 0; e < a.width - c; ++e) St<TO>::st(a.out, to + e, in ? St<TT>::ld(a.table, from + e) * a.scale : none);
       }
-      store_ve<TO, VE>(a.out, i * a.row_stride + c, v, a.past);
     }
   }
 }
 
-bool al16p(const void* p) { return ((uintptr_t)p & 15) == 0; }
-
 // ---- sort -------------------------------------------------------------------------------------
 
-// Rows of the gradient to clear: [row0, row1), 32 to a workgroup.
+// Rows of the gradient to clear: [row0, row1), `rows` to a workgroup (a power of two up to 32, about 64 KB).
 struct ClearRows {
   float* dtable;
   int64_t table_stride, row0, row1;
-  int width, wide, past;
+  int width, rows, past;
 };
-// ZE elements a thread and store; `has`: bits of rows that are left as they are
-template <int ZE>
-__device__ __forceinline__ void clear_word(const ClearRows& a, int64_t row, unsigned has) {
+// workgroup i of those that clear; has: bits of the rows of its word of row bits that are left as they are
+__device__ __forceinline__ void clear_rows(const ClearRows& a, int64_t i, const unsigned* present) {
+  constexpr int ZE = St<float>::VE;
   const float z[ZE] = {};
+  const int64_t first = a.row0 + i * a.rows;
+  const unsigned has = present != nullptr ? present[first / 32] >> (first & 31) : 0;
   int tpr = 1;
   while (tpr < (int)blockDim.x && tpr * ZE < a.width) tpr *= 2;
-  const int rows = blockDim.x / tpr, lane = threadIdx.x & (tpr - 1);
-  for (int r = threadIdx.x / tpr; r < 32; r += rows) {
-    const int64_t v = row + r;
-    if (v >= a.row1 || (has >> r & 1)) continue;
-    for (int c = lane * ZE; c < a.width; c += tpr * ZE) store_ve<float, ZE>(a.dtable, v * a.table_stride + c, z, a.past);
+  const int lane = threadIdx.x & (tpr - 1);
+  for (int r = threadIdx.x / tpr; r < a.rows; r += blockDim.x / tpr) {
+    if (first + r >= a.row1 || (has >> r & 1)) continue;
+    for (int c = lane * ZE; c < a.width; c += tpr * ZE) {
+      const int64_t o = (first + r) * a.table_stride + c;
+      if (c + ZE <= a.width) store_piece<float>(a.dtable, o, z, a.past);
+      else
+        for (int e = 0; e < a.width - c; ++e) a.dtable[o + e] = 0.0f;
+    }
   }
-}
-__device__ __forceinline__ void clear_word(const ClearRows& a, int64_t word, unsigned has) {
-  if (a.wide) clear_word<4>(a, a.row0 + word * 32, has);
-  else clear_word<1>(a, a.row0 + word * 32, has);
 }
 
 struct EmbedSort {
@@ -131,7 +147,7 @@ struct EmbedSort {
 
 __device__ __forceinline__ bool clears_rows(const EmbedSort& a) {
   if (blockIdx.x < a.clear_from) return false;
-  clear_word(a.clear, blockIdx.x - a.clear_from, 0);
+  clear_rows(a.clear, blockIdx.x - a.clear_from, nullptr);
   return true;
 }
 
@@ -375,30 +391,30 @@ struct EmbedSum {
   unsigned* present;           // NULL: no row has tokens
   int64_t n, vocab, tiles, table_stride, row_stride;
   int64_t join_blocks;         // second launch: workgroups that join runs; the others clear rows
-  int width, tpr, run, accumulate, past;
+  int width, tpr, run, accumulate;
   float scale;
   ClearRows clear;             // the rows of the second launch
 };
 
-template <int VE>
-__device__ __forceinline__ void write_row(const EmbedSum& a, int64_t row, int c, const float* acc) {
+__device__ __forceinline__ void write_row(const EmbedSum& a, int64_t row, int c, int left, const float* acc) {
   const int64_t o = row * a.table_stride + c;
   float v[VE];
 #pragma unroll
   for (int e = 0; e < VE; ++e) v[e] = a.scale * acc[e];
   if (a.accumulate) {
     float old[VE];
-    load_ve<float, VE>(a.dtable, o, old);
+    load_ve<float>(a.dtable, o, left, old);
 #pragma unroll
     for (int e = 0; e < VE; ++e) v[e] += old[e];
   }
-  store_ve<float, VE>(a.dtable, o, v, a.past);
+  store_ve<float>(a.dtable, o, left, v);
 }
 
 // Sums of one tile: runs inside the tile are written, a run from the tile before goes to part row 0
 // (also when it goes on behind this tile), one that starts here and goes on to part row 1.  The rows
-// of eight positions are loaded at a time.  UNI: a tile's threads are whole waves.
-template <typename T, int VE, bool UNI>
+// of eight positions are loaded at a time.  UNI: a tile's threads are whole waves; WHOLE: the width is a multiple of VE
+// (without the second set of loads 67 registers a lane instead of 109: 16384 x 2048 138 us against 149).
+template <typename T, bool UNI, bool WHOLE>
 __global__ __launch_bounds__(THREADS) void embed_sum_kernel(EmbedSum a) {
   int sub = threadIdx.x / a.tpr;
   if constexpr (UNI) sub = __builtin_amdgcn_readfirstlane(sub);
@@ -407,6 +423,7 @@ __global__ __launch_bounds__(THREADS) void embed_sum_kernel(EmbedSum a) {
   if (tile >= a.tiles || c >= a.width) return;
   const int64_t s0 = tile * a.run, s1 = s0 + a.run < a.n ? s0 + a.run : a.n;
   const int32_t prev = s0 > 0 ? a.key[s0 - 1] : -1, next = s1 < a.n ? a.key[s1] : -1;
+  const int left = WHOLE ? VE : a.width - c;     // elements from c on
   int32_t cur = a.key[s0];
   float acc[VE];
 #pragma unroll
@@ -414,11 +431,11 @@ __global__ __launch_bounds__(THREADS) void embed_sum_kernel(EmbedSum a) {
   auto flush = [&](bool at_end) {
     if (cur >= a.vocab) return;
     if (cur == prev) {
-      store_ve<float, VE>(a.part, tile * 2 * a.width + c, acc);
+      store_ve<float>(a.part, tile * 2 * a.width + c, left, acc);
     } else {
       if (c == 0 && !a.accumulate) atomicOr(&a.present[cur >> 5], 1u << (cur & 31));
-      if (at_end && cur == next) store_ve<float, VE>(a.part, (tile * 2 + 1) * a.width + c, acc);
-      else write_row<VE>(a, cur, c, acc);
+      if (at_end && cur == next) store_ve<float>(a.part, (tile * 2 + 1) * a.width + c, left, acc);
+      else write_row(a, cur, c, left, acc);
     }
   };
   constexpr int U = 8;
@@ -431,8 +448,13 @@ __global__ __launch_bounds__(THREADS) void embed_sum_kernel(EmbedSum a) {
       k[u] = a.key[i];
       p[u] = a.pos[i];
     }
+    if (left >= VE) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) load_ve<T, VE>(a.dout, (int64_t)p[u] * a.row_stride + c, v[u]);
+      for (int u = 0; u < U; ++u) load_ve<T>(a.dout, (int64_t)p[u] * a.row_stride + c, VE, v[u]);
+    } else {
+#pragma unroll
+      for (int u = 0; u < U; ++u) load_ve<T>(a.dout, (int64_t)p[u] * a.row_stride + c, left, v[u]);
+    }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (s + u >= s1) break;
@@ -452,8 +474,7 @@ __global__ __launch_bounds__(THREADS) void embed_sum_kernel(EmbedSum a) {
 // Second launch.  Its first join_blocks workgroups join the runs over several tiles, by the tile they
 // start in: its part row 1, then the part rows 0 of the tiles up to the one the run ends in; each of
 // the JW groups of 64 threads takes every JW-th of them, the groups' sums are added in order.  The
-// others clear the rows without tokens that the sort's launches left, 32 (a word of `present`) each.
-template <int VE>
+// others clear the rows without tokens that the sort's launches left.
 __global__ __launch_bounds__(THREADS) void embed_join_kernel(EmbedSum a) {
   constexpr int JW = THREADS / 64;
   if (blockIdx.x < a.join_blocks) {
@@ -484,7 +505,7 @@ __global__ __launch_bounds__(THREADS) void embed_join_kernel(EmbedSum a) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int64_t i = r + u * JW < rows ? r + u * JW : r;
-        load_ve<float, VE>(a.part, (i == 0 ? tile * 2 + 1 : (tile + i) * 2) * a.width + c, v[u]);
+        load_ve<float>(a.part, (i == 0 ? tile * 2 + 1 : (tile + i) * 2) * a.width + c, a.width - c, v[u]);
       }
 #pragma unroll
       for (int u = 0; u < U; ++u)
@@ -500,11 +521,10 @@ __global__ __launch_bounds__(THREADS) void embed_join_kernel(EmbedSum a) {
     for (int w = 1; w < JW; ++w)
 #pragma unroll
       for (int e = 0; e < VE; ++e) acc[e] += sum[w][lane][e];
-    write_row<VE>(a, cur, c, acc);
+    write_row(a, cur, c, a.width - c, acc);
     return;
   }
-  const int64_t word = blockIdx.x - a.join_blocks;
-  clear_word(a.clear, word, a.present != nullptr ? a.present[word] : 0);
+  clear_rows(a.clear, blockIdx.x - a.join_blocks, a.present);
 }
 
 constexpr int64_t MAX_GRID = 65536;   // workgroups of the row loops
@@ -523,18 +543,12 @@ int launch_embed_fwd(const pnn_embed_desc& d, const void* table, const void* tok
   a.width = (int)d.width;
   a.token_bytes = d.token_bytes;
   a.scale = d.scale;
-  a.past = d.n * d.width * (d.dtype == PNN_F32 ? 4 : 2) > L2_BYTES;
   const int es = d.dtype == PNN_F32 ? 4 : 2, et = d.table_dtype == PNN_F32 ? 4 : 2;
-  // 8 elements a piece: whole 16-byte pieces on both sides
-  const bool wide = d.width % 8 == 0 && al16p(table) && al16p(out) && d.table_stride * et % 16 == 0 && d.row_stride * es % 16 == 0;
-  a.tpr = threads_per_row(wide ? d.width / 8 : d.width);
+  a.past = d.n * d.width * es > L2_BYTES;
+  a.tpr = threads_per_row(cdiv64(d.width, 16 / es));
   const int64_t grid = cdiv64(d.n, THREADS / a.tpr);
   const dim3 g((unsigned)(grid < MAX_GRID ? grid : MAX_GRID));
-#define FWD(TT, TO)                                                              \
-  do {                                                                           \
-    if (wide) hipLaunchKernelGGL((embed_fwd_kernel<TT, TO, 8>), g, dim3(THREADS), 0, s, a); \
-    else hipLaunchKernelGGL((embed_fwd_kernel<TT, TO, 1>), g, dim3(THREADS), 0, s, a);      \
-  } while (0)
+#define FWD(TT, TO) hipLaunchKernelGGL((embed_fwd_kernel<TT, TO>), g, dim3(THREADS), 0, s, a)
   if (et == 4 && es == 4) FWD(float, float);
   else if (et == 4) FWD(float, uint16_t);
   else if (es == 4) FWD(uint16_t, float);
@@ -556,13 +570,12 @@ int launch_embed_bwd(const pnn_embed_desc& d, const void* dout, const void* toke
   a.passes = w.passes;
   a.words = accumulate ? 0 : w.words;
   a.present = (unsigned*)(base + w.present);
-  const int es = d.dtype == PNN_F32 ? 4 : 2;
-  const bool wide = d.width % 8 == 0 && al16p(dtable) && al16p(dout) && d.table_stride % 4 == 0 && d.row_stride * es % 16 == 0;
   ClearRows clear;
   clear.dtable = dtable;
   clear.table_stride = d.table_stride;
   clear.width = (int)d.width;
-  clear.wide = wide;
+  clear.rows = 32;
+  while (clear.rows > 1 && clear.rows * d.width > 16384) clear.rows /= 2;
   clear.past = d.vocab * d.width * 4 > L2_BYTES;
   int64_t rows = accumulate ? 0 : d.vocab;               // rows not yet taken by a launch that clears them
   // The last rows left go to the launch to come: EMB_CLEAR bytes of them, whole words of row bits, and no more rows in
@@ -578,7 +591,7 @@ int launch_embed_bwd(const pnn_embed_desc& d, const void* dout, const void* toke
     a.clear.row0 = from;
     a.clear.row1 = rows;
     a.clear_from = blocks;
-    const int64_t more = cdiv64(rows - from, 32);
+    const int64_t more = cdiv64(rows - from, clear.rows);
     rows = from;
     return dim3((unsigned)(blocks + more));
   };
@@ -627,35 +640,33 @@ int launch_embed_bwd(const pnn_embed_desc& d, const void* dout, const void* toke
   m.row_stride = d.row_stride;
   m.width = (int)d.width;
   m.accumulate = accumulate != 0;
-  m.past = clear.past;
   m.clear = clear;
   m.clear.row0 = 0;
   m.clear.row1 = rows;
   m.scale = d.scale;
-  const int64_t pieces = wide ? d.width / 8 : d.width;
+  const int64_t pieces = cdiv64(d.width, VE);
   m.tpr = threads_per_row(pieces);
   if (d.n > 0) {
     const dim3 grid((unsigned)cdiv64(w.tiles, THREADS / m.tpr), (unsigned)cdiv64(pieces, m.tpr));
-#define SUMS(T, VE)                                                                                    \
-  do {                                                                                                 \
-    if (m.tpr >= 64) hipLaunchKernelGGL((embed_sum_kernel<T, VE, true>), grid, block, 0, s, m);        \
-    else hipLaunchKernelGGL((embed_sum_kernel<T, VE, false>), grid, block, 0, s, m);                   \
+#define SUMS(T, UNI)                                                                                                \
+  do {                                                                                                              \
+    if (d.width % VE == 0) hipLaunchKernelGGL((embed_sum_kernel<T, UNI, true>), grid, block, 0, s, m);              \
+    else hipLaunchKernelGGL((embed_sum_kernel<T, UNI, false>), grid, block, 0, s, m);                               \
   } while (0)
-    if (es == 4) {
-      if (wide) SUMS(float, 8);
-      else SUMS(float, 1);
+    if (m.tpr >= 64) {
+      if (d.dtype == PNN_F32) SUMS(float, true);
+      else SUMS(uint16_t, true);
     } else {
-      if (wide) SUMS(uint16_t, 8);
-      else SUMS(uint16_t, 1);
+      if (d.dtype == PNN_F32) SUMS(float, false);
+      else SUMS(uint16_t, false);
     }
 #undef SUMS
     if (const hipError_t e = hipGetLastError()) return (int)e;
   }
-  m.join_blocks = (w.tiles > 1 ? w.tiles - 1 : 0) * cdiv64(d.width, 64 * (wide ? 8 : 1));
-  const int64_t blocks = m.join_blocks + cdiv64(rows, 32);
+  m.join_blocks = (w.tiles > 1 ? w.tiles - 1 : 0) * cdiv64(d.width, 64 * VE);
+  const int64_t blocks = m.join_blocks + cdiv64(rows, clear.rows);
   if (blocks == 0) return 0;
-  if (wide) hipLaunchKernelGGL((embed_join_kernel<8>), dim3((unsigned)blocks), block, 0, s, m);
-  else hipLaunchKernelGGL((embed_join_kernel<1>), dim3((unsigned)blocks), block, 0, s, m);
+  hipLaunchKernelGGL(embed_join_kernel, dim3((unsigned)blocks), block, 0, s, m);
   return (int)hipGetLastError();
 }
 

@@ -33,17 +33,49 @@ __device__ __forceinline__ void store_to(P* p, V v, bool past) {
   }
 }
 
-// One 16-byte piece of T at element i, two bf16 to a conversion.
+// 16-byte pieces of T that need no more than T's alignment (global memory takes unaligned vectors on this device)
+template <typename T> struct Piece;
+template <> struct Piece<float> {
+  typedef float Vec __attribute__((ext_vector_type(4)));
+  typedef Vec Mem __attribute__((aligned(4)));
+};
+template <> struct Piece<uint16_t> {
+  typedef uint32_t Vec __attribute__((ext_vector_type(4)));
+  typedef Vec Mem __attribute__((aligned(2)));
+};
+template <typename T>
+__device__ __forceinline__ void load_piece(const void* base, int64_t i, float* v) {
+  const typename Piece<T>::Vec u = *(const typename Piece<T>::Mem*)((const T*)base + i);
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = u[e];
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[2 * e] = __uint_as_float(u[e] << 16);
+      v[2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
+    }
+  }
+}
+// past: as in store_to
 template <typename T>
 __device__ __forceinline__ void store_piece(void* base, int64_t i, const float* v, bool past) {
+  typedef typename Piece<T>::Vec Vec;
+  Vec u;
   if constexpr (sizeof(T) == 4) {
-    typedef float f32x4_ __attribute__((ext_vector_type(4)));
-    store_to((f32x4_*)((float*)base + i), f32x4_{v[0], v[1], v[2], v[3]}, past);
+    u = Vec{v[0], v[1], v[2], v[3]};
   } else {
     typedef float f32x8 __attribute__((ext_vector_type(8)));
     typedef __bf16 bf16x8_ __attribute__((ext_vector_type(8)));
     const f32x8 f = {v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]};
-    store_to((bf16x8_*)((uint16_t*)base + i), __builtin_convertvector(f, bf16x8_), past);
+    u = __builtin_bit_cast(Vec, __builtin_convertvector(f, bf16x8_));
+  }
+  if (past) {
+    asm volatile("");
+    __builtin_nontemporal_store(u, (typename Piece<T>::Mem*)((T*)base + i));
+    asm volatile("");
+  } else {
+    *(typename Piece<T>::Mem*)((T*)base + i) = u;
   }
 }
 
