@@ -68,11 +68,13 @@ __device__ __forceinline__ void gate_of(float g, float& f, float& keep) {
 template <typename T, int VEC> struct Raw;
 template <> struct Raw<uint16_t, 1> {
   typedef uint16_t U;
+  typedef U Mem;
   __device__ static __forceinline__ void get(U u, float* v) { v[0] = bf2f(u); }
   __device__ static __forceinline__ U put(const float* v) { return f2bf(v[0]); }
 };
 template <> struct Raw<uint16_t, 2> {
   typedef uint32_t U;
+  typedef U Mem __attribute__((aligned(2)));   // rows may start on any element
   __device__ static __forceinline__ void get(U u, float* v) {
     v[0] = __uint_as_float(u << 16);
     v[1] = __uint_as_float(u & 0xffff0000u);
@@ -85,6 +87,7 @@ template <> struct Raw<uint16_t, 2> {
 };
 template <> struct Raw<float, 1> {
   typedef float U;
+  typedef U Mem;
   __device__ static __forceinline__ void get(U u, float* v) { v[0] = u; }
   __device__ static __forceinline__ U put(const float* v) { return v[0]; }
 };
@@ -94,14 +97,14 @@ template <> struct Raw<float, 1> {
 template <typename T, int VEC, int S>
 __device__ __forceinline__ void load_steps(typename Raw<T, VEC>::U (&r)[S], const void* base, const pnn_seq_stride& st,
                                            int64_t b, int t0, int end, int c, typename Raw<T, VEC>::U none) {
-  typedef typename Raw<T, VEC>::U U;
+  typedef const typename Raw<T, VEC>::Mem Mem;
   const T* p = (const T*)base + (b * st.batch + (int64_t)t0 * st.step);
   if (t0 + S <= end) {
 #pragma unroll
-    for (int s = 0; s < S; ++s) r[s] = *at<const U>(p + s * st.step, c * sizeof(T));
+    for (int s = 0; s < S; ++s) r[s] = *at<Mem>(p + s * st.step, c * sizeof(T));
   } else {
 #pragma unroll
-    for (int s = 0; s < S; ++s) r[s] = t0 + s < end ? *at<const U>(p + s * st.step, c * sizeof(T)) : none;
+    for (int s = 0; s < S; ++s) r[s] = t0 + s < end ? *at<Mem>(p + s * st.step, c * sizeof(T)) : none;
   }
 }
 
@@ -126,7 +129,10 @@ __device__ __forceinline__ Place place(const Dims& d) {
   p.wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   p.c = ((int)(p.chain - p.b * d.groups) * 64 + p.lane) * VEC;
   p.on = p.c < d.channels;
-  p.cc = p.on ? p.c : d.channels - VEC;    // lanes past the end load what the last one does
+  // lanes past the end load what the last one does; of an odd number of channels the last pair overlaps the one before
+  // it, and both lanes store the same bits
+  p.cc = p.c + VEC <= d.channels ? p.c : d.channels - VEC;
+  p.c = p.cc;
   return p;
 }
 
@@ -243,7 +249,7 @@ __device__ __forceinline__ void gates(const typename Raw<T, VEC>::U (&rx)[S], co
 // ---- forward --------------------------------------------------------------------------------
 
 template <typename T, int VEC, int NW, bool DEALT>
-__global__ __launch_bounds__(64 * NW) void scan_fwd_kernel(Dims d, ScanArgs a) {
+__global__ __launch_bounds__(64 * NW, NW == 8 ? 4 : 1) void scan_fwd_kernel(Dims d, ScanArgs a) {
   typedef typename Raw<T, VEC>::U U;
   constexpr int L = NW * FS;
   __shared__ float2 part[2][NW][64][VEC];
@@ -351,7 +357,7 @@ __global__ __launch_bounds__(64 * NW) void scan_fwd_kernel(Dims d, ScanArgs a) {
       for (int s = 0; s < FS; ++s) {
 #pragma unroll
         for (int e = 0; e < VEC; ++e) h[e] = fmaf(f[s][e], h[e], b[s][e]);
-        if (p.on) store_to(at<U>(hp + (int64_t)(t + s) * d.h.step, p.c * sizeof(T)), Raw<T, VEC>::put(h), d.past);
+        if (p.on) store_to(at<typename Raw<T, VEC>::Mem>(hp + (int64_t)(t + s) * d.h.step, p.c * sizeof(T)), Raw<T, VEC>::put(h), d.past);
       }
     } else {
 #pragma unroll
@@ -362,7 +368,7 @@ __global__ __launch_bounds__(64 * NW) void scan_fwd_kernel(Dims d, ScanArgs a) {
           h[e] = fmaf(f[s][e], h[e], b[s][e]);
           o[e] = t + s < len ? h[e] : 0.0f;
         }
-        if (p.on && t + s < end) *at<U>(hp + (int64_t)(t + s) * d.h.step, p.c * sizeof(T)) = Raw<T, VEC>::put(o);
+        if (p.on && t + s < end) *at<typename Raw<T, VEC>::Mem>(hp + (int64_t)(t + s) * d.h.step, p.c * sizeof(T)) = Raw<T, VEC>::put(o);
       }
     }
     last = k == d.tiles - 1;
@@ -379,10 +385,10 @@ __global__ __launch_bounds__(64 * NW) void scan_fwd_kernel(Dims d, ScanArgs a) {
 
 // Tile k of the chain is the k-th from the sequence's end.
 template <typename T, int VEC, int NW, bool DEALT>
-__global__ __launch_bounds__(64 * NW) void scan_bwd_kernel(Dims d, ScanArgs a) {
+__global__ __launch_bounds__(64 * NW, NW == 8 ? 4 : 1) void scan_bwd_kernel(Dims d, ScanArgs a) {
   typedef typename Raw<T, VEC>::U U;
   constexpr int L = NW * BS;
-  static_assert(NW < SCAN_NW || L == SCAN_CHUNK, "tiles start at kept states (fewer waves: one tile)");
+  static_assert(NW < 8 || L % SCAN_CHUNK == 0, "tiles start at kept states (fewer waves: one tile)");
   __shared__ float2 part[2][NW][64][VEC];
   __shared__ float back[2][NW][64][VEC];
   __shared__ float2 look[DEALT ? LOOK * 64 * VEC : 1];
@@ -399,7 +405,7 @@ __global__ __launch_bounds__(64 * NW) void scan_bwd_kernel(Dims d, ScanArgs a) {
     load_steps<T, VEC, BS>(rg, a.gate, d.gate, p.b, t, len, p.cc, U(0));
     load_steps<T, VEC, BS>(rd, a.dh, d.dh, p.b, t, len, p.cc, U(0));
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) state[e] = a.states[(p.b * d.chunks + tile) * d.channels + p.cc + e];
+    for (int e = 0; e < VEC; ++e) state[e] = a.states[(p.b * d.chunks + tile * L / SCAN_CHUNK) * d.channels + p.cc + e];
   };
   if (tiles.cur < d.tiles) load(tiles.cur);
   // the gradient from behind the tile at hand; DEALT: of wave 0, from behind tile `known`
@@ -532,8 +538,8 @@ __global__ __launch_bounds__(64 * NW) void scan_bwd_kernel(Dims d, ScanArgs a) {
         c[e] = f[s][e] * G;
       }
       if (p.on && t + s < end) {
-        store_to(at<U>(xp + (int64_t)(t + s) * d.dx.step, p.c * sizeof(T)), Raw<T, VEC>::put(ox), d.past);
-        store_to(at<U>(gp + (int64_t)(t + s) * d.dgate.step, p.c * sizeof(T)), Raw<T, VEC>::put(og), d.past);
+        store_to(at<typename Raw<T, VEC>::Mem>(xp + (int64_t)(t + s) * d.dx.step, p.c * sizeof(T)), Raw<T, VEC>::put(ox), d.past);
+        store_to(at<typename Raw<T, VEC>::Mem>(gp + (int64_t)(t + s) * d.dgate.step, p.c * sizeof(T)), Raw<T, VEC>::put(og), d.past);
       }
     }
     last = k == d.tiles - 1;
@@ -545,9 +551,6 @@ __global__ __launch_bounds__(64 * NW) void scan_bwd_kernel(Dims d, ScanArgs a) {
 #pragma unroll
     for (int e = 0; e < VEC; ++e) a.dh0[p.b * d.channels + p.c + e] = carry[e];
 }
-
-bool even(const pnn_seq_stride& s) { return s.batch % 2 == 0 && s.step % 2 == 0; }
-bool al4(const void* p) { return ((uintptr_t)p & 3) == 0; }
 
 Dims dims(const pnn_scan_desc& d, const ScanArgs& a, int vec, int tile) {
   Dims m;
@@ -581,14 +584,13 @@ void begin(const Dims& m, const float* from, int64_t states, int vec, hipStream_
 }  // namespace
 
 int launch_scan_fwd(const pnn_scan_desc& d, const ScanArgs& a, hipStream_t s) {
-  const int nw = d.length <= FS ? 1 : d.length <= 4 * FS ? 4 : 16;
-  const bool pair = d.dtype == PNN_BF16 && scan_pairs(d, false) && al4(a.x) && al4(a.gate) && al4(a.h) && even(d.x) &&
-                    even(d.gate) && even(d.h);
+  const bool pair = scan_pairs(d, false);
+  const int nw = scan_waves(d.batch * cdiv64(d.channels, pair ? 128 : 64), d.length, FS);
 #define FWD(T, VEC, NW)                                                                                             \
   do {                                                                                                              \
     const Dims m = dims(d, a, VEC, NW * FS);                                                                        \
     const dim3 grid((unsigned)(m.chains * m.dealt)), block(64 * NW);                                                \
-    if constexpr (NW == SCAN_NW) /* fewer waves: a single tile */                                                   \
+    if constexpr (NW == SCAN_NW) /* fewer waves: a single tile, or enough sequences */                              \
       if (m.dealt > 1) {                                                                                            \
         begin(m, a.h0, d.batch * d.channels, VEC, s);                                                               \
         hipLaunchKernelGGL((scan_fwd_kernel<T, VEC, NW, true>), grid, block, 0, s, m, a);                           \
@@ -600,6 +602,7 @@ int launch_scan_fwd(const pnn_scan_desc& d, const ScanArgs& a, hipStream_t s) {
   do {                                \
     if (nw == 1) FWD(T, VEC, 1);      \
     else if (nw == 4) FWD(T, VEC, 4); \
+    else if (nw == 8) FWD(T, VEC, 8); \
     else FWD(T, VEC, SCAN_NW);             \
   } while (0)
   if (d.dtype == PNN_F32) FWD_NW(float, 1);
@@ -611,14 +614,13 @@ int launch_scan_fwd(const pnn_scan_desc& d, const ScanArgs& a, hipStream_t s) {
 }
 
 int launch_scan_bwd(const pnn_scan_desc& d, const ScanArgs& a, hipStream_t s) {
-  const int nw = d.length <= BS ? 1 : d.length <= 4 * BS ? 4 : 16;
-  const bool pair = d.dtype == PNN_BF16 && scan_pairs(d, true) && al4(a.x) && al4(a.gate) && al4(a.dh) && al4(a.dx) &&
-                    al4(a.dgate) && even(d.x) && even(d.gate) && even(d.dh) && even(d.dx) && even(d.dgate);
+  const bool pair = scan_pairs(d, true);
+  const int nw = scan_waves(d.batch * cdiv64(d.channels, pair ? 128 : 64), d.length, BS);
 #define BWD(T, VEC, NW)                                                                                             \
   do {                                                                                                              \
     const Dims m = dims(d, a, VEC, NW * BS);                                                                        \
     const dim3 grid((unsigned)(m.chains * m.dealt)), block(64 * NW);                                                \
-    if constexpr (NW == SCAN_NW) /* fewer waves: a single tile */                                                   \
+    if constexpr (NW == SCAN_NW && VEC == 1) /* pairs: enough sequences */                                          \
       if (m.dealt > 1) {                                                                                            \
         begin(m, a.dhT, d.batch * d.channels, VEC, s);                                                               \
         hipLaunchKernelGGL((scan_bwd_kernel<T, VEC, NW, true>), grid, block, 0, s, m, a);                           \
@@ -630,6 +632,7 @@ int launch_scan_bwd(const pnn_scan_desc& d, const ScanArgs& a, hipStream_t s) {
   do {                                \
     if (nw == 1) BWD(T, VEC, 1);      \
     else if (nw == 4) BWD(T, VEC, 4); \
+    else if (nw == 8) BWD(T, VEC, 8); \
     else BWD(T, VEC, SCAN_NW);             \
   } while (0)
   if (d.dtype == PNN_F32) BWD_NW(float, 1);

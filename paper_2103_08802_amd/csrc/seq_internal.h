@@ -71,7 +71,7 @@ int launch_embed_bwd(const pnn_embed_desc& d, const void* dout, const void* toke
 // ---- recurrence ----
 constexpr int SCAN_FS = 16, SCAN_BS = 8;   // steps of a wave in a tile, forward and backward
 constexpr int SCAN_NW = 16;                // waves of a tile of a long sequence
-constexpr int SCAN_CHUNK = SCAN_NW * SCAN_BS;   // steps from one kept state to the next
+constexpr int SCAN_CHUNK = 8 * SCAN_BS;         // steps from one kept state to the next: the shorter tiles of the backward
 constexpr int64_t SCAN_WGS = 256;          // workgroups that fill the device (one of 16 waves a CU)
 struct ScanArgs {
   const void *x, *gate;
@@ -87,6 +87,13 @@ struct ScanArgs {
   void* ws;
 };
 inline int64_t scan_chunks(const pnn_scan_desc& d) { return cdiv64(d.length, SCAN_CHUNK); }
+// Waves of a tile: as many as the sequence has work for; 8, of which a CU holds two workgroups, where there are two
+// workgroups a CU.
+inline int scan_waves(int64_t chains, int64_t length, int steps) {
+  if (length <= steps) return 1;
+  if (length <= 4 * steps) return 4;
+  return length <= 8 * steps || chains >= 2 * SCAN_WGS ? 8 : SCAN_NW;
+}
 // Workgroups a sequence's tiles are dealt to, given the channel groups of the whole batch: as many as fill the device.
 // Two tiles already pay (4 x 512 steps of 512 channels, backward: 12 us against 21 by one workgroup after the other).
 inline int scan_dealt(int64_t chains, int64_t tiles) {
@@ -97,7 +104,7 @@ inline int scan_dealt(int64_t chains, int64_t tiles) {
 // twice the workgroups, unless even those are too few: the forward, whose dealt tiles cost more than its bytes, then
 // takes pairs again (65536 steps of 1024 channels: 104 us against 119; backward 253 against 202).
 inline bool scan_pairs(const pnn_scan_desc& d, bool backward) {
-  if (d.channels % 2 != 0 || d.channels <= 64) return false;
+  if (d.dtype != PNN_BF16 || d.channels <= 64) return false;
   return d.batch * cdiv64(d.channels, 128) >= SCAN_WGS || (!backward && d.batch * cdiv64(d.channels, 64) < SCAN_WGS);
 }
 // Workspace of dealt tiles: tickets, first states, the tiles' (A, B) (64 vec pairs each)

@@ -165,6 +165,10 @@ SCAN = [
     (1, 5003, 9, "f32", "dense", None, True, 0),
     (100, 1500, 30, "bf16", "halves", "ragged", True, 0),        # several tiles for each of two workgroups
     (40, 2311, 66, "f32", "dense", "ragged", True, 0),           # two channel groups, three workgroups each
+    (300, 40, 131, "bf16", "halves", "ragged", True, 1),         # pairs of an odd number of channels, rows on odd elements
+    (260, 150, 66, "bf16", "time", "ragged", True, 0),
+    (520, 300, 5, "f32", "dense", "ragged", True, 0),            # eight-wave tiles, several of them
+    (600, 70, 65, "bf16", "dense", None, False, 0),
 ]
 
 
