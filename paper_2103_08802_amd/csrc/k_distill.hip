@@ -11,6 +11,12 @@
 //
 // Rows may start anywhere: the whole pieces between the first and the last 16-byte boundary are the
 // row's body, the elements before and behind (fewer than two pieces) go to one thread each.
+//
+// Bound: HBM (bf16, 4096 x 65536 classes, 64 entries, labels: 204 us, 1.07 GB at 5.3 TB/s, what a large
+// copy reaches), with two rows to a compute unit so that one's exponentials (18 vector operations an
+// element in all, two of them exponentials) run while the other's pieces are on their way; rows read
+// twice reach 4.1 TB/s of that count (2048 x 131072 float: 529 us).  Few long rows: a row's latency, 18 us
+// at 128000 classes.
 #include "device_common.h"
 #include "seq_device.h"
 #include "seq_internal.h"

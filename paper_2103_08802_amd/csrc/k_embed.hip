@@ -5,6 +5,12 @@
 // terms stand together in token order; tiles of sorted positions are summed by one group of
 // threads each, whatever the tokens' distribution, and the runs that cross tiles are joined from the
 // tiles' partial rows in a second launch, in tile order.  No floating-point atomics.
+//
+// Bound: HBM, for few tokens the dependent launches.  bf16, 16384 tokens, 2048 columns, 65536 rows:
+// forward 16.5 us (92 MB; frequent rows come from the caches), gradient 137 us (604 MB at 4.4 TB/s, 480 MB
+// of it zeros): sort 33 us in four launches, which clear 130 MB meanwhile, sums 23, joins and the rest
+// of the zeros 75.  65536 tokens, 1024 columns, 8192 rows: 82 us a batch, 28 of it the sort, 40 the sums
+// (134 MB), 13 the joins.
 #include "device_common.h"
 #include "seq_device.h"
 #include "seq_internal.h"
