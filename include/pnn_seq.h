@@ -24,7 +24,8 @@
  *   - Results do not depend on timing: no sum is formed in an order that varies from run to run.
  *   - Return value: PNN_OK or a negative pnn_status; on error nothing has been enqueued, except for
  *     PNN_ERR_HIP.  PNN_ERR_TOO_LARGE: sizes or offsets beyond what the kernels index (2^28 samples,
- *     2^23 pieces of 32 tokens x 64 elements or of 32 table rows, 2^31 - 1 classes, 2^30 steps, 2^21 times 64 channels in a
+ *     2^22 pieces of 32 tokens x 64 elements, 32 table rows or 16384 elements
+ *     of the table, 2^31 - 1 classes, 2^30 steps, 2^21 times 64 channels in a
  *     batch, 2^60 elements from a tensor's first to its last).
  */
 #ifndef PNN_SEQ_H
@@ -126,7 +127,8 @@ typedef struct {
  *     loss = alpha tau^2 sum_k p_k (log p_k - log q_{index_k})  +  (1 - alpha) (-log s_label)
  *     dlogits_v = scale weight (alpha tau (q_v - sum_{k: index_k = v} p_k) + (1 - alpha) (s_v - [v = label]))
  * The first term is zero for a row without entries (all indices below 0, or all its logits -inf), the
- * second without labels (NULL) or for a label below 0.  An entry whose p is 0 adds nothing.  A class
+ * second without labels (NULL) or for a label below 0; a term whose weight (alpha, 1 - alpha) is 0 is
+ * left out, its indices or labels unread.  An entry whose p is 0 adds nothing.  A class
  * may stand in several entries.  An index or label not below `classes` makes the row's loss and
  * gradient NaN.  weight (float[rows], nullable): factor of the row's gradient, not of its loss.
  * loss: float[rows].  dlogits (nullable: loss only) may be logits itself (with the same stride).

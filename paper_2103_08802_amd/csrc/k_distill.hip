@@ -13,7 +13,7 @@
 // row's body, the elements before and behind (fewer than two pieces) go to one thread each.
 //
 // Bound: HBM (bf16, 4096 x 65536 classes, 64 entries, labels: 204 us, 1.07 GB at 5.3 TB/s, what a large
-// copy reaches), with two rows to a compute unit so that one's exponentials (18 vector operations an
+// copy reaches), with two rows to a compute unit so that one's exponentials (20 vector operations an
 // element in all, two of them exponentials) run while the other's pieces are on their way; rows read
 // twice reach 4.1 TB/s of that count (2048 x 131072 float: 529 us).  Few long rows: a row's latency, 18 us
 // at 128000 classes.
@@ -26,7 +26,7 @@ namespace pnn {
 namespace {
 
 constexpr int64_t MAX_GRID = 1 << 20;   // rows of a launch
-constexpr float LOG2E = 1.44269504f, LN2 = 0.693147181f;
+constexpr float LOG2E = 1.44269504f;
 
 struct Distill {
   const void *z, *t;
@@ -46,23 +46,24 @@ enum { ONE = 0, SQUARE = 1, FOURTH = 2, BOTH = 3 };
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// A row's reference point: m times the factors of the exponents, rounded once.  Exponents are formed as
-// fma(z, k, -km), everywhere the same, so the rounding of km is a common factor of a row's exponentials
-// and drops out of every quotient; logarithms of the sums are taken relative to km as well.
+// A row's reference point: its maximum and log2(e) / tau (ONE: the factor of the only softmax).  The difference
+// comes first: an exponent as fma(z, k, -round(k m)) is an operation less, but its rounding error grows with the
+// logits themselves and is infinite where all of them are the type's lowest value.
 struct Ref {
-  float kq, mq, ms;   // log2(e) / tau (ONE: of the only softmax), kq m, log2(e) m (BOTH)
+  float m, kq;
 };
 // exponentials of z / tau and z about the reference point
 template <int MODE>
 __device__ __forceinline__ void exps(float z, const Ref& r, float& eq, float& es) {
-  eq = exp2_(fmaf(z, r.kq, -r.mq));
+  const float d = z - r.m;
+  eq = exp2_(d * r.kq);
   if constexpr (MODE == ONE) es = eq;
   if constexpr (MODE == SQUARE) es = eq * eq;
   if constexpr (MODE == FOURTH) {
     const float e2 = eq * eq;
     es = e2 * e2;
   }
-  if constexpr (MODE == BOTH) es = exp2_(fmaf(z, LOG2E, -r.ms));
+  if constexpr (MODE == BOTH) es = exp2_(d * LOG2E);
 }
 // four elements' exponentials added to the sums; the four exponentials stand together, ahead of their uses
 template <int MODE>
@@ -78,22 +79,13 @@ __device__ __forceinline__ void add_exps(const float* z, const Ref& r, float& sq
     if constexpr (MODE == BOTH) ss += es[e];
   }
 }
-// exponents (base 2) of those two
-__device__ __forceinline__ float exponent_q(float z, const Ref& r) { return fmaf(z, r.kq, -r.mq); }
-template <int MODE>
-__device__ __forceinline__ float exponent_s(float z, const Ref& r) {
-  return MODE == BOTH ? fmaf(z, LOG2E, -r.ms) : (MODE == SQUARE ? 2.0f : MODE == FOURTH ? 4.0f : 1.0f) * fmaf(z, r.kq, -r.mq);
-}
-template <int MODE>
-__device__ __forceinline__ Ref ref_at(float m, float kq) {
-  return Ref{kq, m * kq, MODE == BOTH ? m * LOG2E : 0.0f};
-}
 // sums about one reference point as sums about another
 template <int MODE>
 __device__ __forceinline__ void move_sums(const Ref& from, const Ref& to, float& sq, float& ss) {
-  const float e = exp2_(from.mq - to.mq);
-  sq *= e;
-  ss *= MODE == BOTH ? exp2_(from.ms - to.ms) : MODE == SQUARE ? e * e : MODE == FOURTH ? e * e * (e * e) : e;
+  float eq, es;
+  exps<MODE>(from.m, to, eq, es);
+  sq *= eq;
+  ss *= es;
 }
 
 // A row of T as a body of whole 16-byte pieces and single elements before (`head`) and behind it
@@ -197,7 +189,7 @@ __global__ __launch_bounds__(NT, NC == 8 ? 8 : 1) void distill_kernel(Distill a)
   }
   // maximum of the row; with the row read twice also the thread's sums about its own maximum
   float m = edge, sq = 0.0f, ss = 0.0f;
-  Ref ref = {kq, 0.0f, 0.0f};                      // a thread that has seen nothing but -inf: sums stay 0
+  Ref ref = {0.0f, kq};                            // a thread that has seen nothing but -inf: sums stay 0
   if constexpr (NC > 0) {
 #pragma unroll
     for (int j = 0; j < NC; ++j) {
@@ -208,7 +200,7 @@ __global__ __launch_bounds__(NT, NC == 8 ? 8 : 1) void distill_kernel(Distill a)
     }
   } else {
     if (m != -INFINITY) {
-      ref = ref_at<MODE>(m, kq);
+      ref = Ref{m, kq};
       exps<MODE>(m, ref, sq, ss);
     }
     for (int c = tid; c < r.pieces; c += NT) {
@@ -218,7 +210,7 @@ __global__ __launch_bounds__(NT, NC == 8 ? 8 : 1) void distill_kernel(Distill a)
 #pragma unroll
       for (int e = 1; e < VE; ++e) cm = fmaxf(cm, v.v[e]);
       if (cm > m) {
-        const Ref next = ref_at<MODE>(cm, kq);
+        const Ref next = {cm, kq};
         if (m != -INFINITY) move_sums<MODE>(ref, next, sq, ss);
         ref = next;
         m = cm;
@@ -249,7 +241,7 @@ __global__ __launch_bounds__(NT, NC == 8 ? 8 : 1) void distill_kernel(Distill a)
   if (all & 2) tm = __builtin_nanf("");
   const bool some = tm != -INFINITY;             // an entry with a finite (or NaN) teacher logit
   const Ref own_ref = ref;
-  ref = ref_at<MODE>(m, kq);
+  ref = Ref{m, kq};
   // sums of exponentials: of the row about m, of the teacher's entries about tm
   if constexpr (NC > 0) {
     float eq, es;
@@ -302,13 +294,13 @@ __global__ __launch_bounds__(NT, NC == 8 ? 8 : 1) void distill_kernel(Distill a)
     ts += wp[w];
   }
   if constexpr (MODE == ONE) ss = sq;
-  // log p_k - log q_k = (t_k - tm) / tau - log ts - ln2 (exponent of z_k) + log sq
+  // log p_k - log q_k = (t_k - tm) / tau - log ts - (z_k - m) / tau + log sq
   const float inv_ts = 1.0f / ts, lqt = logf(sq) - logf(ts);
   float kl = 0.0f;
   for (int k = tid; k < a.top; k += NT) {
     if (!some || ei[k] < 0) continue;
     const float p = exp2_((et[k] - tm) * kt) * inv_ts;
-    if (p != 0.0f) kl += p * (fmaf(et[k] - tm, inv_tau, -LN2 * exponent_q(ez[k], ref)) + lqt);
+    if (p != 0.0f) kl += p * (((et[k] - tm) - (ez[k] - m)) * inv_tau + lqt);
   }
   const bool hard = y >= 0;
   float g = a.scale * (a.weight != nullptr ? a.weight[row] : 1.0f);
@@ -361,7 +353,7 @@ __global__ __launch_bounds__(NT, NC == 8 ? 8 : 1) void distill_kernel(Distill a)
 #pragma unroll
     for (int w = 0; w < NWV; ++w) l += wk[w];
     l *= a.alpha * a.tau * a.tau;
-    if (hard) l += (1.0f - a.alpha) * (logf(ss) - LN2 * exponent_s<MODE>(ez[a.top], ref));
+    if (hard) l += (1.0f - a.alpha) * (logf(ss) - (ez[a.top] - m));
     a.loss[row] = bad ? __builtin_nanf("") : l;
   }
   if (a.dz != nullptr && !zero && !bad) {

@@ -242,6 +242,41 @@ def test_scan(B, T, D, dtype, layout, lens, state, lead):
         assert torch.equal(place, dh0.t)
 
 
+def test_scans_side_by_side():
+    """Sequences whose tiles are dealt to every compute unit, on three streams at once: the bits each gives alone."""
+    seq = _seq()
+    g = _gen(21)
+    B, T, D = 1, 9001, 200
+    runs = []
+    for i in range(3):
+        x, dh = (torch.randn(B, T, D, generator=g).cuda() for _ in range(2))
+        gate = (torch.randn(B, T, D, generator=g) + torch.rand(D, generator=g) * 8 - 2).cuda()
+        h, dx, dg = torch.empty_like(x), torch.empty_like(x), torch.empty_like(x)
+        d = seq.scan_desc(x, gate, h, dh, dx, dg)
+        n, w = seq.pnn_scan_sizes(d)
+        states, ws = torch.empty(n // 4, device="cuda"), torch.empty(w, dtype=torch.uint8, device="cuda")
+        runs.append((d, x, gate, h, dh, dx, dg, states, ws, torch.cuda.Stream()))
+
+    def go(r):
+        d, x, gate, h, dh, dx, dg, states, ws, _ = r
+        seq.pnn_scan_fwd(d, x, gate, None, None, h, None, states, ws, _stream())
+        seq.pnn_scan_bwd(d, x, gate, None, states, dh, None, dx, dg, None, ws, _stream())
+
+    alone = []
+    for r in runs:
+        go(r)
+        torch.cuda.synchronize()
+        alone.append([t.clone() for t in (r[3], r[5], r[6])])
+    for _ in range(5):
+        for r in runs:
+            with torch.cuda.stream(r[-1]):
+                go(r)
+    torch.cuda.synchronize()
+    for r, want in zip(runs, alone):
+        for a, b in zip((r[3], r[5], r[6]), want):
+            assert torch.equal(a, b)
+
+
 def test_scan_step_by_step_is_the_sequence():
     """Single steps with the state in place give the states of the whole sequence, up to the roundings of either."""
     seq = _seq()
@@ -410,6 +445,35 @@ def test_distill_rows_without_terms_ignore_their_logits():
     z[0] = -math.inf
     seq.pnn_distill_fwd_bwd(d, z, index, teacher, labels, None, loss, dz, _stream())
     assert math.isnan(loss[0]) and bool(torch.isnan(dz[0]).all()) and not dz[1:].any()
+
+
+@pytest.mark.parametrize("V", [50, 9000, 140003])          # one wave, a workgroup, a row read twice
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("tau", [1.0, 2.0, 4.0, 3.0])
+def test_distill_rows_of_huge_logits(V, dtype, tau):
+    """Rows whose logits are all the type's lowest value are uniform; huge ones of any sign keep their differences."""
+    seq = _seq()
+    g = _gen(V)
+    low = torch.finfo(R.DT[dtype]).min
+    z = torch.randn(6, V, generator=g)
+    z[0] = low
+    z[1] = -low / 4
+    z[2] += 1e6
+    z[3] *= 1e30
+    z[4], z[4, 7] = low, 0.25
+    z[5, ::2] = low
+    index = torch.randint(0, V // 2, (6, 4), generator=g, dtype=torch.int32) * 2 + 1
+    labels = index[:, 1].clone()
+    index[3], labels[3] = z[3].argmax().item(), z[3].argmax().item()
+    index[4], labels[4] = 7, 7
+    teacher = torch.randn(6, 4, generator=g)
+    zs = z.cuda().to(R.DT[dtype])
+    loss, dz = torch.empty(6, device="cuda"), torch.empty_like(zs)
+    d = seq.distill_desc(zs, teacher.cuda(), dz, tau, 0.5, 1.0)
+    seq.pnn_distill_fwd_bwd(d, zs, index.cuda(), teacher.cuda(), labels.cuda(), None, loss, dz, _stream())
+    want = R.distill(zs, index, teacher, labels, None, d.temperature, d.alpha, 1.0)
+    R.within(loss, want[0], want[1], "f32")
+    R.within(dz, want[2], want[3], dtype)
 
 
 def test_distill_gradient_is_the_difference_quotient():
