@@ -20,8 +20,8 @@
 // Bound: HBM.  bf16, 8 x 2048 steps of 2048 channels: forward 42 us (201 MB, 4.8 TB/s; a large copy
 // reaches 5.2), backward 80 us (335 MB, 4.2 TB/s).  One sequence of 65536 steps, 1024 channels: forward
 // 99 us (403 MB, 4.1 TB/s; with a first launch that sums up ranges and reads x and gate twice 139),
-// backward 205 us (671 MB): there a tile of 128 steps costs a look back of two to three microseconds,
-// which the loads in flight (they return in order, so it waits for them) only partly hide.
+// backward 203 us (671 MB): there a tile of 128 steps costs a look back of two to three microseconds
+// that nothing hides, as one workgroup fills a compute unit's registers.
 #include "device_common.h"
 #include "seq_device.h"
 #include "seq_internal.h"
@@ -449,7 +449,8 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 4 : 1) void scan_bwd_kernel(Dims
     }
 #pragma unroll
     for (int e = 0; e < VEC; ++e) h[e] = state[e];
-    if (tiles.next < d.tiles) load(tiles.next);
+    if constexpr (!DEALT)
+      if (tiles.next < d.tiles) load(tiles.next);
     float A[VEC], B[VEC], C[VEC];
 #pragma unroll
     for (int e = 0; e < VEC; ++e) {
@@ -498,6 +499,9 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 4 : 1) void scan_bwd_kernel(Dims
         for (int e = 0; e < VEC; ++e) publish(d.sum + ((p.chain * d.tiles + k) * 64 + p.lane) * VEC + e, A[e], C[e]);
       }
       look_back<VEC, NW>(d, p, known, k, carry, look, gave_up);
+      // only now: loads return in order, so the look back would wait for these (30000 steps 195 us with the forward, 184
+      // so; the forward's longer tiles are better off with the loads ahead)
+      if (tiles.next < d.tiles) load(tiles.next);
       if (p.wave == 0)
 #pragma unroll
         for (int e = 0; e < VEC; ++e) {
