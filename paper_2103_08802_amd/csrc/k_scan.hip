@@ -133,11 +133,12 @@ __device__ __forceinline__ Place place(const Dims& d) {
   p.b = p.chain / d.groups;
   p.lane = threadIdx.x & 63;
   p.wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  p.c = ((int)(p.chain - p.b * d.groups) * 64 + p.lane) * VEC;
-  p.on = p.c < d.channels;
+  const ScanGroup r = scan_group(d.channels, (int)(p.chain - p.b * d.groups), VEC);
+  p.c = r.first + p.lane * VEC;
+  p.on = p.c < r.end;
   // lanes past the end load what the last one does; of an odd number of channels the last pair overlaps the one before
-  // it, and both lanes store the same bits
-  p.cc = p.c + VEC <= d.channels ? p.c : d.channels - VEC;
+  // it, in the same wave, and both lanes store the same bits
+  p.cc = p.c + VEC <= r.end ? p.c : r.end - VEC;
   p.c = p.cc;
   return p;
 }

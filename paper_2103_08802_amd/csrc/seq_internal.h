@@ -107,6 +107,22 @@ inline bool scan_pairs(const pnn_scan_desc& d, bool backward) {
   if (d.dtype != PNN_BF16 || d.channels <= 64) return false;
   return d.batch * cdiv64(d.channels, 128) >= SCAN_WGS || (!backward && d.batch * cdiv64(d.channels, 64) < SCAN_WGS);
 }
+// Channels [first, end) of a channel group, 64 lanes of vec channels.  Groups share none, so that a state may stand in
+// place (hT = h0, dh0 = dhT): one group's workgroups may end before the next one's read theirs.  Of an odd number of
+// channels the last two lanes' pairs meet in a channel, so where the last group had only one, it takes the pair before
+// from its neighbour too (vec = 2 has more than 64 channels, hence two groups there).
+struct ScanGroup {
+  int first, end;
+};
+__host__ __device__ inline ScanGroup scan_group(int channels, int group, int vec) {
+  const int size = 64 * vec, full = (group + 1) * size;
+  ScanGroup r = {group * size, full < channels ? full : channels};
+  if (vec == 2 && channels % size == 1) {
+    if (r.end == channels) r.first -= 2;
+    else if (full == channels - 1) r.end -= 2;
+  }
+  return r;
+}
 // Workspace of dealt tiles: tickets, first states, the tiles' (A, B) (64 vec pairs each)
 struct ScanWs {
   int64_t tickets, first, sum, bytes;
