@@ -164,7 +164,7 @@ __global__ __launch_bounds__(NT, NC == 8 ? 8 : 1) void distill_kernel(Distill a)
     }
   }
   const bool has_edge = tid < r.edges();
-  const int ve = r.edge(tid);
+  const int ve = has_edge ? r.edge(tid) : 0;
   const float edge = has_edge ? St<T>::ld(r.p, ve) : -INFINITY;
   for (int h = tid; h <= a.hash_mask; h += NT) table[h] = -1;
   if (tid == 0) twice = listed = 0;
@@ -333,7 +333,7 @@ __global__ __launch_bounds__(NT, NC == 8 ? 8 : 1) void distill_kernel(Distill a)
       }
     };
     if (zero) {
-      for (int v = tid; v < a.classes; v += NT) St<T>::st(dp, v, 0.0f);
+      for (unsigned v = tid; v < (unsigned)a.classes; v += NT) St<T>::st(dp, v, 0.0f);   // v may pass 2^31
     } else if constexpr (NC > 0) {
 #pragma unroll
       for (int j = 0; j < NC; ++j) {
