@@ -548,10 +548,19 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 4 : 1) void scan_bwd_kernel(Dims
         og[e] = ox[e] * f[s][e] * x[s][e];
         c[e] = f[s][e] * G;
       }
-      if (p.on && t + s < end) {
+      if (p.on && t + s < len) {
         store_to(at<typename Raw<T, VEC>::Mem>(xp + (int64_t)(t + s) * d.dx.step, p.c * sizeof(T)), Raw<T, VEC>::put(ox), d.past);
         store_to(at<typename Raw<T, VEC>::Mem>(gp + (int64_t)(t + s) * d.dgate.step, p.c * sizeof(T)), Raw<T, VEC>::put(og), d.past);
       }
+    }
+    if (t + BS > len) {        // behind the sequence's end: zeros, whatever passes through
+#pragma unroll
+      for (int s = 0; s < BS; ++s)
+        if (p.on && t + s >= len && t + s < end) {
+          const typename Raw<T, VEC>::U zero = 0;
+          store_to(at<typename Raw<T, VEC>::Mem>(xp + (int64_t)(t + s) * d.dx.step, p.c * sizeof(T)), zero, d.past);
+          store_to(at<typename Raw<T, VEC>::Mem>(gp + (int64_t)(t + s) * d.dgate.step, p.c * sizeof(T)), zero, d.past);
+        }
     }
     last = k == d.tiles - 1;
     tiles.cur = tiles.next;
