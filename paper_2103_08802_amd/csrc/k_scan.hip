@@ -43,13 +43,15 @@ struct Dims {
   float2* sum;              // [chains][tiles][64 VEC]: (A, B) of a tile, READY set in A once published
 };
 
-// f = sigmoid(g) and keep = 1 - f = exp(-g) f, each to about an ulp (keep is not formed by subtraction).
-// g is held between -87 and 100, where both are constant to the last bit and exp(-g) is finite, by
-// minimum and maximum that keep NaN.  exp(-g) = 2^t (1 + d): t = -g log2(e) rounded, d the rest of that
+// f = sigmoid(g) and keep = 1 - f = exp(-g) f, each to about an ulp (keep is not formed by subtraction), or zero where it
+// is under about 1.6e-38 (f below g = -87, keep above 87.3): gates of -inf and +inf replace and hold a state exactly,
+// however large it is.  g is held between -87 and 100, where exp(-g) is finite, by minimum and maximum that keep NaN.
+// exp(-g) = 2^t (1 + d): t = -g log2(e) rounded, d the rest of that
 // product to first order.  A bf16 g has 8 bits, so its product with the leading 16 bits of log2(e) is
 // exact; for float the rounding is recovered by a fused multiply-add, and the reciprocal is refined.
 template <typename T>
 __device__ __forceinline__ void gate_of(float g, float& f, float& keep) {
+  const bool closed = g < -87.0f;
   g = __builtin_elementwise_minimum(__builtin_elementwise_maximum(g, -87.0f), 100.0f);
   float e, r;
   if constexpr (sizeof(T) == 2) {
@@ -66,7 +68,7 @@ __device__ __forceinline__ void gate_of(float g, float& f, float& keep) {
     r = __builtin_amdgcn_rcpf(d);
     r = fmaf(fmaf(-d, r, 1.0f), r, r);
   }
-  f = r;
+  f = closed ? 0.0f : r;
   keep = e * r;
 }
 

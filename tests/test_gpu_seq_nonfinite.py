@@ -1,5 +1,5 @@
 """The recurrence at the edges of its numbers: states and gradients that are not finite stay out of the steps behind a
-sequence's end."""
+sequence's end, and gates of plus and minus infinity hold or replace a state exactly, however large it is."""
 import math
 
 import pytest
@@ -56,3 +56,22 @@ def test_steps_behind_the_end_stay_zero(B, T, D, dtype, what):
         assert not got[name][behind].any(), name            # NaN counts as true
     for name in got:
         assert torch.equal(got[name][..., 1:], want[name][..., 1:]), name
+
+
+@pytest.mark.parametrize("B,T,D,dtype", SHAPES)
+def test_infinite_gates_hold_and_replace(B, T, D, dtype):
+    """f is 1 and 1 - f is 0 for a gate of +inf, the other way round for -inf: a state of 1e38 is gone after the one,
+    an input of 1e38 never arrives with the other, and neither has a gradient from what it leaves out."""
+    x, gate, dh, lengths, h0, dhT = _inputs(B, T, D, dtype, B + T + D + 1)
+    g = torch.Generator().manual_seed(B * T)
+    kind = torch.randint(0, 6, gate.shape, generator=g).cuda()
+    kind[:, 0, 0], kind[:, 0, 1] = 0, 1
+    gate[kind == 0], gate[kind == 1] = -math.inf, math.inf
+    x[kind == 1] *= 1e37
+    h0 *= 1e37
+    dh *= 2.0 ** -7
+    dhT *= 2.0 ** -7
+    got = _run(x, gate, lengths, h0, dh, dhT)
+    ref = R.scan(x, gate, lengths, h0, dh, dhT)
+    for name in got:
+        R.within(got[name], *ref[name], dtype if name in ("h", "dx", "dgate") else "f32")
