@@ -132,7 +132,7 @@ typedef struct {
  * may stand in several entries.  An index or label not below `classes` makes the row's loss and
  * gradient NaN.  weight (float[rows], nullable): factor of the row's gradient, not of its loss.
  * loss: float[rows].  dlogits (nullable: loss only) may be logits itself (with the same stride).
- * PNN_ERR_VALUE: tau not above zero, or tau, 1 / tau, alpha tau^2 or scale not finite. */
+ * PNN_ERR_VALUE: tau not above zero, or tau, log2(e) / tau, alpha tau^2 or scale not finite. */
 pnn_status pnn_distill_fwd_bwd(const pnn_distill_desc* d, const void* logits, const int32_t* index,
                                const void* teacher, const int32_t* labels, const float* weight, float* loss,
                                void* dlogits, void* stream);

@@ -183,7 +183,8 @@ pnn_status pnn_distill_fwd_bwd(const pnn_distill_desc* d, const void* logits, co
   if (dlogits != nullptr)
     if (pnn_status e = rows_ok(d->rows, d->grad_stride, d->classes, true)) return e;
   const float tau = d->temperature;
-  if (!isfinite(tau) || !(tau > 0.0f) || !isfinite(1.0f / tau) || !isfinite(d->alpha * tau * tau) || !isfinite(d->scale))
+  // the kernel's largest factor is log2(e) / tau
+  if (!isfinite(tau) || !(tau > 0.0f) || !isfinite(1.44269504f / tau) || !isfinite(d->alpha * tau * tau) || !isfinite(d->scale))
     return PNN_ERR_VALUE;
   if (d->rows == 0) return PNN_OK;
   if (logits == nullptr || loss == nullptr || (d->top > 0 && (index == nullptr || teacher == nullptr)))
