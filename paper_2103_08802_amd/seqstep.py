@@ -127,11 +127,12 @@ class SequenceModel:
         self.tokens.copy_(tokens.view_as(self.tokens))
         self.forward(keep=False)
         self.token1.copy_(t.mm(self.h[:, -1], self.w.t()).argmax(1))
-        out = [self.token1.clone()]
-        for _ in range(steps - 1):
-            self.answer_step()
-            out.append(self.token1.clone())
-        return t.stack(out, 1)
+        out = t.empty(self.batch, steps, dtype=t.int64, device=self.dev)
+        for i in range(steps):
+            if i > 0:
+                self.answer_step()
+            out[:, i] = self.token1
+        return out
 
 
 def main():
