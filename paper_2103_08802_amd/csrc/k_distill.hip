@@ -101,8 +101,8 @@ struct Row {
     pieces = (classes - head) / St<T>::VE;
   }
   __device__ __forceinline__ int edges() const { return classes - pieces * St<T>::VE; }   // < 2 VE
-  // class of edge element i
-  __device__ __forceinline__ int edge(int i) const { return i < head ? i : i + pieces * St<T>::VE; }
+  // class of edge element i; unsigned, as it is formed past the edges too and may pass 2^31 there
+  __device__ __forceinline__ unsigned edge(unsigned i) const { return i < (unsigned)head ? i : i + pieces * St<T>::VE; }
 };
 
 template <typename T>
@@ -164,7 +164,7 @@ __global__ __launch_bounds__(NT, NC == 8 ? 8 : 1) void distill_kernel(Distill a)
     }
   }
   const bool has_edge = tid < r.edges();
-  const int ve = has_edge ? r.edge(tid) : 0;
+  const unsigned ve = r.edge(tid);
   const float edge = has_edge ? St<T>::ld(r.p, ve) : -INFINITY;
   for (int h = tid; h <= a.hash_mask; h += NT) table[h] = -1;
   if (tid == 0) twice = listed = 0;
