@@ -540,22 +540,30 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 4 : 1) void scan_bwd_kernel(Dims
         x[s][e] = h[e] - x[s][e];
         h[e] = next;
       }
+    auto gradients = [&](int stop) {
 #pragma unroll
-    for (int s = BS - 1; s >= 0; --s) {
-      float ox[VEC], og[VEC];
+      for (int s = BS - 1; s >= 0; --s) {
+        float ox[VEC], og[VEC];
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        const float G = g[s][e] + c[e];
-        ox[e] = G * keep[s][e];
-        og[e] = ox[e] * f[s][e] * x[s][e];
-        c[e] = f[s][e] * G;
+        for (int e = 0; e < VEC; ++e) {
+          const float G = g[s][e] + c[e];
+          ox[e] = G * keep[s][e];
+          og[e] = ox[e] * f[s][e] * x[s][e];
+          c[e] = f[s][e] * G;
+        }
+        if (p.on && t + s < stop) {
+          store_to(at<typename Raw<T, VEC>::Mem>(xp + (int64_t)(t + s) * d.dx.step, p.c * sizeof(T)), Raw<T, VEC>::put(ox), d.past);
+          store_to(at<typename Raw<T, VEC>::Mem>(gp + (int64_t)(t + s) * d.dgate.step, p.c * sizeof(T)), Raw<T, VEC>::put(og), d.past);
+        }
       }
-      if (p.on && t + s < len) {
-        store_to(at<typename Raw<T, VEC>::Mem>(xp + (int64_t)(t + s) * d.dx.step, p.c * sizeof(T)), Raw<T, VEC>::put(ox), d.past);
-        store_to(at<typename Raw<T, VEC>::Mem>(gp + (int64_t)(t + s) * d.dgate.step, p.c * sizeof(T)), Raw<T, VEC>::put(og), d.past);
-      }
-    }
-    if (t + BS > len) {        // behind the sequence's end: zeros, whatever passes through
+    };
+    // whole waves without a comparison a step, waves behind the end without the sums (16 x 2048 x 1024: 75.4 us where one
+    // form for all took 77.1; ragged 76.0 and 78.6)
+    if (t + BS <= len) {
+      gradients(t + BS);
+    } else {
+      if (t < len) gradients(len);
+      // behind the sequence's end: zeros, whatever passes through
 #pragma unroll
       for (int s = 0; s < BS; ++s)
         if (p.on && t + s >= len && t + s < end) {
