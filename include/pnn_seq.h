@@ -20,6 +20,9 @@
  *     on 16-byte boundaries (pointer and strides) are moved in 16-byte pieces and run fastest.
  *   - An index (token, class) below zero means "none"; one past the end is the caller's mistake and
  *     turns the row it belongs to into NaN.
+ *   - An output shares no element with an input, a workspace or another output, unless its entry point
+ *     says that it may stand in an input's place.  Equal pointers are refused (PNN_ERR_SHAPE); whether
+ *     tensors overlap otherwise is not looked at.
  *   - Empty problems are valid (pointers of tensors without elements may be NULL).
  *   - Results do not depend on timing: no sum is formed in an order that varies from run to run.
  *   - Return value: PNN_OK or a negative pnn_status; on error nothing has been enqueued, except for
@@ -51,7 +54,8 @@ typedef struct {
   float scale;
 } pnn_embed_desc;
 
-/* out[i] = scale * table[tokens[i]]; zeros for a token below 0, NaN for one not below vocab. */
+/* out[i] = scale * table[tokens[i]]; zeros for a token below 0, NaN for one not below vocab.
+ * PNN_ERR_VALUE (also below): scale not finite. */
 pnn_status pnn_embed_fwd(const pnn_embed_desc* d, const void* table, const void* tokens, void* out,
                          void* stream);
 
@@ -61,7 +65,8 @@ pnn_status pnn_embed_workspace_size(const pnn_embed_desc* d, size_t* bytes);
 /* dtable[v] = scale * sum over the tokens i with tokens[i] = v of dout[i], for every row v (rows
  * without tokens become zero); with accumulate != 0 the sum is added to dtable[v] and rows without
  * tokens are left as they are.  Tokens outside the table have no gradient.  The tokens are sorted
- * (stably, on the device), so that a row's sum runs in token order. */
+ * (stably, on the device) and a row's sum has one order whatever the run: in token order within tiles of
+ * sorted tokens, the tiles' sums in a fixed order after that. */
 pnn_status pnn_embed_bwd(const pnn_embed_desc* d, const void* dout, const void* tokens, float* dtable,
                          int accumulate, void* workspace, void* stream);
 
@@ -91,7 +96,8 @@ pnn_status pnn_scan_sizes(const pnn_scan_desc* d, size_t* states, size_t* worksp
  * the nearer end).  hT (nullable, float [batch][channels]): the state after the last step; may be h0
  * itself.  states (nullable): kept for pnn_scan_bwd.  h0: float [batch][channels].
  * One step at a time (length 1, hT = h0) is the form for answering: the state stays in place.
- * h may not be x or gate. */
+ * h may not be x or gate.  f_t or 1 - f_t is 0 where it is below about 1.6e-38.  A state that is not
+ * finite makes what follows it in its sequence and channel not finite (infinite or NaN). */
 pnn_status pnn_scan_fwd(const pnn_scan_desc* d, const void* x, const void* gate, const int32_t* lengths,
                         const float* h0, void* h, float* hT, float* states, void* workspace, void* stream);
 

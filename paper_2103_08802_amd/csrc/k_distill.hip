@@ -12,11 +12,11 @@
 // Rows may start anywhere: the whole pieces between the first and the last 16-byte boundary are the
 // row's body, the elements before and behind (fewer than two pieces) go to one thread each.
 //
-// Bound: HBM (bf16, 4096 x 65536 classes, 64 entries, labels: 204 us, 1.07 GB at 5.3 TB/s, what a large
-// copy reaches), with two rows to a compute unit so that one's exponentials (20 vector operations an
-// element in all, two of them exponentials) run while the other's pieces are on their way; rows read
-// twice reach 4.1 TB/s of that count (2048 x 131072 float: 529 us).  Few long rows: a row's latency, 18 us
-// at 128000 classes.
+// Bound: HBM (bf16, 4096 x 65536 classes, 64 entries, labels: 205 us, 1.07 GB at 5.2 TB/s, what a large
+// copy reaches; the loss alone 127 us), with two rows to a compute unit so that one's exponentials (20 vector
+// operations an element in all, two of them exponentials) run while the other's pieces are on their way; rows
+// read twice reach 4.1 TB/s of that count (2048 x 131072 float: 528 us, 2048 x 151936 bf16: 296 us).  Few long
+// rows: a row's latency, 18 us at 128000 classes.
 #include "device_common.h"
 #include "seq_device.h"
 #include "seq_internal.h"
@@ -41,7 +41,9 @@ struct Distill {
 };
 
 // Which exponentials a row needs: one softmax (tau = 1, or only one of the two terms), both with
-// softmax(z)'s exponentials as squares or fourth powers of those of z / 2 or z / 4, or both apart.
+// softmax(z)'s exponentials as squares or fourth powers of those of z / 2 or z / 4, or both apart.  4096 x 65536
+// bf16: SQUARE 204 us, FOURTH 213, and BOTH, which would serve their temperatures too, 224 (tau 0.5) to 231 (3).
+// FOURTH and BOTH spill four registers with eight bf16 pieces a thread.
 enum { ONE = 0, SQUARE = 1, FOURTH = 2, BOTH = 3 };
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }

@@ -18,10 +18,11 @@
 // unpublished one waits for nothing, hence every wait ends, however few workgroups run at a time.
 //
 // Bound: HBM.  bf16, 8 x 2048 steps of 2048 channels: forward 42 us (201 MB, 4.8 TB/s; a large copy
-// reaches 5.2), backward 80 us (335 MB, 4.2 TB/s).  One sequence of 65536 steps, 1024 channels: forward
-// 99 us (403 MB, 4.1 TB/s; with a first launch that sums up ranges and reads x and gate twice 139),
-// backward 203 us (671 MB): there a tile of 128 steps costs a look back of two to three microseconds
-// that nothing hides, as one workgroup fills a compute unit's registers.
+// reaches 5.2), backward 81 us (335 MB, 4.2 TB/s); float 65 and 145 us (403 and 671 MB, part of it from
+// the caches).  One sequence of 65536 steps, 1024 channels: forward 99 us (403 MB, 4.1 TB/s; with a first
+// launch that sums up ranges and reads x and gate twice 139), backward 206 us (671 MB): there a tile of
+// 128 steps costs a look back of two to three microseconds that nothing hides, as one workgroup fills a
+// compute unit's registers.
 #include "device_common.h"
 #include "seq_device.h"
 #include "seq_internal.h"

@@ -46,7 +46,7 @@ pnn_status embed_ok(const pnn_embed_desc* d) {
   if (!type_ok(d->dtype) || !type_ok(d->table_dtype) || (d->token_bytes != 4 && d->token_bytes != 8))
     return PNN_ERR_DTYPE;
   if (d->n < 0 || d->vocab < 0 || d->width < 0) return PNN_ERR_SHAPE;
-  // grids: at most a workgroup for every 32 tokens x 64 elements, for every 32 rows and for every 8192 elements of the table
+  // grids: at most a workgroup for every 32 tokens x 64 elements, for every 32 rows and for every 16384 elements of the table
   if (d->n > (1 << 28) || d->vocab >= MAX_COUNT || d->width > (1 << 23)) return PNN_ERR_TOO_LARGE;
   if (cdiv64(d->n, 32) * cdiv64(d->width, 64) + cdiv64(d->vocab, 32) + cdiv64(d->vocab * d->width, 16384) > (1 << 22)) return PNN_ERR_TOO_LARGE;
   if (pnn_status e = rows_ok(d->vocab, d->table_stride, d->width, false)) return e;

@@ -7,7 +7,7 @@ logits, and answering one token at a time.
     loss, dL/dlogits                     teacher's top logits and labels             pnn_distill_fwd_bwd
     dL/dh = dL/dlogits W, dL/dW          library products
     dL/dx, dL/dgate                                                                  pnn_scan_bwd
-    dL/dtable                            token order                                 pnn_embed_bwd
+    dL/dtable                            one order of every sum                      pnn_embed_bwd
 
 The recurrence is the evolution the parareal construction splits into intervals, here in time: intervals from a zero
 state in parallel, a sequential chain over their ends, a correction of every interval (eqs. (rk) - (tildey)), with a
@@ -26,9 +26,9 @@ from . import seq as Q
 class SequenceModel:
     """Device state of the model and its training step for ``batch`` sequences of ``length`` tokens.
 
-    dtype: "bf16" or "f32", the storage type of the parameters, activations and their gradients (the table's and W's
-    gradients are float).  Tokens below zero are padding; they take part in no loss if their labels are below zero and
-    their rows have no teacher entries."""
+    dtype: "bf16" or "f32", the storage type of the parameters, activations and their gradients (the table's gradient
+    is float; W's, a library product, is rounded to the storage type).  Tokens below zero are padding; they take part
+    in no loss if their labels are below zero and their rows have no teacher entries."""
 
     def __init__(self, vocab, channels, batch, length, top, dtype="bf16", temperature=2.0, alpha=0.5, seed=0,
                  device="cuda"):
