@@ -1,9 +1,11 @@
 /*
- * libpnn, operators for sequence models: token embedding, gated linear recurrence, and the loss that
- * trains towards a teacher's top logits.
+ * libpnn, operators for sequence models: token embedding, gated linear recurrence, linear attention with
+ * a decay for each head, norms around a block, and the losses that train towards a teacher's top logits
+ * or by the model's own answers.
  *
- * A sequence model takes token ids through pnn_embed_fwd, runs pnn_scan_fwd along the sequence and is
- * trained by pnn_distill_fwd_bwd; pnn_scan_bwd and pnn_embed_bwd take the gradient back.  They need no
+ * A sequence model takes token ids through pnn_embed_fwd, runs pnn_scan_fwd or, in blocks between
+ * pnn_norm_fwd, pnn_linattn_fwd along the sequence and is trained by pnn_distill_fwd_bwd or
+ * pnn_policy_fwd_bwd; the _bwd entry points take the gradient back.  They need no
  * plan: each call takes a description of its tensors (filled once, reusable) and device pointers.
  *
  * Conventions for every entry point (as in pnn.h, except for alignment)
@@ -142,6 +144,56 @@ typedef struct {
 pnn_status pnn_distill_fwd_bwd(const pnn_distill_desc* d, const void* logits, const int32_t* index,
                                const void* teacher, const int32_t* labels, const float* weight, float* loss,
                                void* dlogits, void* stream);
+
+/* ---- linear attention with a decay for each head ---------------------------------------------- */
+
+/* strides of a [batch][length][heads][width] tensor, in elements */
+typedef struct {
+  int64_t batch; /* from sequence to sequence */
+  int64_t step;  /* from step to step */
+  int64_t head;  /* from head to head */
+} pnn_head_stride;
+
+typedef struct {
+  int dtype;               /* pnn_dtype of q, k, v, o and their gradients */
+  int64_t batch, length;
+  int64_t heads;           /* of q and o */
+  int64_t kv_heads;        /* of k and v: divides heads, head h takes k and v of h / (heads / kv_heads) */
+  int64_t key_width;       /* elements of a head of q and k, 1 .. PNN_LINATTN_MAX_WIDTH */
+  int64_t value_width;     /* elements of a head of v and o, likewise */
+  pnn_head_stride q, k, v, o;           /* forward */
+  pnn_head_stride dout, dq, dk, dv;     /* backward (not looked at by the forward) */
+  float scale;
+} pnn_linattn_desc;
+
+#define PNN_LINATTN_MAX_WIDTH 256
+
+/* Bytes of workspace of either direction (0: none, the pointer may be NULL). */
+pnn_status pnn_linattn_sizes(const pnn_linattn_desc* d, size_t* forward, size_t* backward);
+
+/* Per sequence and head, with lambda = exp(log_decay[head]):
+ *     S_t = lambda S_{t-1} + k_t v_t^T,   o_t = scale q_t^T S_t,   S_{-1} = s0 (zero when s0 is NULL)
+ * log_decay: float[heads], each at most 0 (0: nothing is forgotten; -inf: all but the step's own term); one that is
+ * positive or NaN makes its head's outputs NaN.  lengths as in pnn_scan_fwd: steps behind a sequence's end are not
+ * looked at, their o is zero and they leave the state as it is.  s0, sT (nullable): float
+ * [batch][heads][key_width][value_width], sT the state after the last step; may be s0 itself.  One step at a time
+ * (length 1, sT = s0) is the form for answering.  o may not be q, k or v.  A q, k or v that is not finite makes
+ * outputs of its own step and, for k and v, of later ones not finite (infinite or NaN), none of earlier steps.
+ * bf16: products that a step's output is a sum of take the weighted q k and the state rounded to bf16; the state
+ * itself is a float sum of terms within 2^-16 of their values. */
+pnn_status pnn_linattn_fwd(const pnn_linattn_desc* d, const void* q, const void* k, const void* v,
+                           const float* log_decay, const int32_t* lengths, const float* s0, void* o, float* sT,
+                           void* workspace, void* stream);
+
+/* The gradients, from dout and (nullable) dsT = dL/dsT, with Z_t = scale q_t dout_t^T + lambda Z_{t+1} and dsT (not
+ * decayed) added at the last step:
+ *     dq_t = scale S_t dout_t,   dk_t = Z_t v_t,   dv_t = Z_t^T k_t,   ds0 = lambda Z_0
+ * dk and dv are summed over the heads that share them, in the heads' order.  log_decay has no gradient.  q, k, v, lengths
+ * and s0 as in the forward; the states in between are formed again.  Steps behind a sequence's end get zero gradients.
+ * ds0 (nullable) may be neither dsT nor s0.  dq, dk and dv may not be q, k, v, dout or one another. */
+pnn_status pnn_linattn_bwd(const pnn_linattn_desc* d, const void* q, const void* k, const void* v,
+                           const float* log_decay, const int32_t* lengths, const float* s0, const void* dout,
+                           const float* dsT, void* dq, void* dk, void* dv, float* ds0, void* workspace, void* stream);
 
 #ifdef __cplusplus
 }

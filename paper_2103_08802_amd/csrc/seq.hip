@@ -66,6 +66,48 @@ pnn_status scan_ok(const pnn_scan_desc* d) {
   return PNN_OK;
 }
 
+// a [batch][length][heads][width] tensor, as seq_ok: of an output, each stride in ascending order holds all that is
+// inside it
+pnn_status heads_ok(const pnn_linattn_desc* d, const pnn_head_stride& s, int64_t heads, int64_t width, bool out) {
+  if (s.batch < 0 || s.step < 0 || s.head < 0) return PNN_ERR_SHAPE;
+  int64_t count[3] = {d->batch, d->length, heads}, stride[3] = {s.batch, s.step, s.head};
+  for (int i = 0; i < 2; ++i)
+    for (int j = 0; j < 2; ++j)
+      if (stride[j] > stride[j + 1]) {
+        const int64_t c = count[j], t = stride[j];
+        count[j] = count[j + 1], stride[j] = stride[j + 1];
+        count[j + 1] = c, stride[j + 1] = t;
+      }
+  __int128 inside = width;
+  for (int i = 0; i < 3; ++i) {
+    if (count[i] <= 1) continue;
+    if (out && stride[i] < inside) return PNN_ERR_SHAPE;
+    inside += (__int128)(count[i] - 1) * stride[i];
+    if (inside > (__int128)MAX_SPAN) return PNN_ERR_TOO_LARGE;
+  }
+  return PNN_OK;
+}
+
+pnn_status linattn_ok(const pnn_linattn_desc* d) {
+  if (d == nullptr) return PNN_ERR_NULL;
+  if (!type_ok(d->dtype)) return PNN_ERR_DTYPE;
+  if (d->batch < 0 || d->length < 0 || d->heads < 1 || d->kv_heads < 1 || d->heads % d->kv_heads != 0 ||
+      d->key_width < 1 || d->value_width < 1)
+    return PNN_ERR_SHAPE;
+  if (d->key_width > LIN_MAX_WIDTH || d->value_width > LIN_MAX_WIDTH || d->length > (1 << 30) || d->heads > (1 << 20) ||
+      d->batch > (1 << 20) || d->batch * d->heads > (1 << 20) ||
+      (__int128)d->batch * d->heads * d->length > ((__int128)1 << 30))
+    return PNN_ERR_TOO_LARGE;
+  if (!isfinite(d->scale)) return PNN_ERR_VALUE;
+  return PNN_OK;
+}
+
+pnn_status linattn_in_ok(const pnn_linattn_desc* d) {
+  if (pnn_status e = heads_ok(d, d->q, d->heads, d->key_width, false)) return e;
+  if (pnn_status e = heads_ok(d, d->k, d->kv_heads, d->key_width, false)) return e;
+  return heads_ok(d, d->v, d->kv_heads, d->value_width, false);
+}
+
 }  // namespace
 
 extern "C" {
@@ -196,6 +238,68 @@ pnn_status pnn_distill_fwd_bwd(const pnn_distill_desc* d, const void* logits, co
   if (dlogits == logits && d->rows > 1 && d->grad_stride != d->logit_stride) return PNN_ERR_SHAPE;
   return launch_distill(*d, logits, index, teacher, labels, weight, loss, dlogits, (hipStream_t)stream) ? PNN_ERR_HIP
                                                                                                         : PNN_OK;
+}
+
+pnn_status pnn_linattn_sizes(const pnn_linattn_desc* d, size_t* forward, size_t* backward) {
+  if (forward == nullptr || backward == nullptr) return PNN_ERR_NULL;
+  if (pnn_status e = linattn_ok(d)) return e;
+  *forward = (size_t)lin_fwd_bytes(*d);
+  *backward = (size_t)lin_bwd(*d).bytes;
+  return PNN_OK;
+}
+
+pnn_status pnn_linattn_fwd(const pnn_linattn_desc* d, const void* q, const void* k, const void* v,
+                           const float* log_decay, const int32_t* lengths, const float* s0, void* o, float* sT,
+                           void* workspace, void* stream) {
+  if (pnn_status e = linattn_ok(d)) return e;
+  if (pnn_status e = linattn_in_ok(d)) return e;
+  if (pnn_status e = heads_ok(d, d->o, d->heads, d->value_width, true)) return e;
+  if (d->batch == 0) return PNN_OK;
+  if (log_decay == nullptr || (d->length > 0 && (q == nullptr || k == nullptr || v == nullptr || o == nullptr)) ||
+      (workspace == nullptr && lin_fwd_bytes(*d) > 0))
+    return PNN_ERR_NULL;
+  const int es = type_size(d->dtype);
+  if (!aligned(q, es) || !aligned(k, es) || !aligned(v, es) || !aligned(o, es) || !aligned(log_decay, 4) ||
+      !aligned(lengths, 4) || !aligned(s0, 4) || !aligned(sT, 4) || !aligned(workspace, 256))
+    return PNN_ERR_ALIGN;
+  if (d->length > 0 && (o == q || o == k || o == v)) return PNN_ERR_SHAPE;
+  return launch_linattn_fwd(*d, q, k, v, log_decay, lengths, s0, o, sT, workspace, (hipStream_t)stream) ? PNN_ERR_HIP
+                                                                                                        : PNN_OK;
+}
+
+pnn_status pnn_linattn_bwd(const pnn_linattn_desc* d, const void* q, const void* k, const void* v,
+                           const float* log_decay, const int32_t* lengths, const float* s0, const void* dout,
+                           const float* dsT, void* dq, void* dk, void* dv, float* ds0, void* workspace, void* stream) {
+  if (pnn_status e = linattn_ok(d)) return e;
+  if (pnn_status e = linattn_in_ok(d)) return e;
+  if (pnn_status e = heads_ok(d, d->dout, d->heads, d->value_width, false)) return e;
+  if (pnn_status e = heads_ok(d, d->dq, d->heads, d->key_width, true)) return e;
+  if (pnn_status e = heads_ok(d, d->dk, d->kv_heads, d->key_width, true)) return e;
+  if (pnn_status e = heads_ok(d, d->dv, d->kv_heads, d->value_width, true)) return e;
+  if (d->batch == 0) return PNN_OK;
+  if (log_decay == nullptr ||
+      (d->length > 0 && (q == nullptr || k == nullptr || v == nullptr || dout == nullptr || dq == nullptr ||
+                         dk == nullptr || dv == nullptr)) ||
+      (workspace == nullptr && lin_bwd(*d).bytes > 0))
+    return PNN_ERR_NULL;
+  const int es = type_size(d->dtype);
+  if (!aligned(q, es) || !aligned(k, es) || !aligned(v, es) || !aligned(dout, es) || !aligned(dq, es) ||
+      !aligned(dk, es) || !aligned(dv, es) || !aligned(log_decay, 4) || !aligned(lengths, 4) || !aligned(s0, 4) ||
+      !aligned(dsT, 4) || !aligned(ds0, 4) || !aligned(workspace, 256))
+    return PNN_ERR_ALIGN;
+  if (ds0 != nullptr && (ds0 == dsT || ds0 == s0)) return PNN_ERR_SHAPE;
+  if (d->length > 0) {
+    const void *in[4] = {q, k, v, dout}, *out[3] = {dq, dk, dv};
+    for (int i = 0; i < 3; ++i) {
+      if (out[i] == out[(i + 1) % 3]) return PNN_ERR_SHAPE;
+      for (int j = 0; j < 4; ++j)
+        if (out[i] == in[j]) return PNN_ERR_SHAPE;
+    }
+  }
+  return launch_linattn_bwd(*d, q, k, v, log_decay, lengths, s0, dout, dsT, dq, dk, dv, ds0, workspace,
+                            (hipStream_t)stream)
+             ? PNN_ERR_HIP
+             : PNN_OK;
 }
 
 }  // extern "C"

@@ -154,4 +154,68 @@ int launch_scan_bwd(const pnn_scan_desc& d, const ScanArgs& a, hipStream_t s);
 int launch_distill(const pnn_distill_desc& d, const void* logits, const int32_t* index, const void* teacher,
                    const int32_t* labels, const float* weight, float* loss, void* dlogits, hipStream_t s);
 
+// ---- linear attention ----
+constexpr int LIN_MAX_WIDTH = PNN_LINATTN_MAX_WIDTH;
+constexpr int64_t LIN_WGS = 256;           // workgroups below which sequences are cut into segments
+// steps of a chunk, by the bytes of an element and the padded inner width: what fits two workgroups into a CU's LDS
+constexpr int lin_chunk(int size, int pad) { return size == 2 && pad <= 128 ? 64 : 32; }
+// How one of the sums runs: inner width padded to `pad`, 64 x tiles value columns to a workgroup, segments of a sequence
+struct LinShape {
+  int pad, tiles, blocks, segments, seg_chunks;
+  int64_t bytes;                           // of the segments' states
+};
+inline LinShape lin_shape(const pnn_linattn_desc& d, int64_t inner, int64_t value, int roles) {
+  LinShape p;
+  p.pad = inner <= 64 ? 64 : inner <= 128 ? 128 : 256;
+  p.tiles = value <= 64 || p.pad == 256 ? 1 : 2;
+  p.blocks = (int)cdiv64(value, 64 * p.tiles);
+  const int64_t chunks = cdiv64(d.length, lin_chunk(d.dtype == PNN_F32 ? 4 : 2, p.pad));
+  const int64_t wgs = d.batch * d.heads * p.blocks * roles;
+  int64_t seg = 1;
+  if (wgs > 0 && wgs < LIN_WGS) {
+    seg = cdiv64(2 * LIN_WGS, wgs);
+    if (seg > chunks / 4) seg = chunks / 4;
+    if (seg < 1) seg = 1;
+  }
+  p.seg_chunks = (int)(chunks > 0 ? cdiv64(chunks, seg) : 1);
+  p.segments = (int)(chunks > 0 ? cdiv64(chunks, p.seg_chunks) : 1);
+  p.bytes = p.segments > 1 ? d.batch * d.heads * p.segments * p.blocks * p.pad * 64 * p.tiles * 4 : 0;
+  return p;
+}
+inline int64_t lin_fwd_bytes(const pnn_linattn_desc& d) {
+  return d.length == 1 ? 0 : lin_shape(d, d.key_width, d.value_width, 1).bytes;
+}
+inline pnn_head_stride lin_dense(const pnn_linattn_desc& d, int64_t width) {
+  return pnn_head_stride{d.length * d.heads * width, d.heads * width, width};
+}
+// Workspace of the backward: the three sums' segments; gradients of single heads where keys and values are shared
+struct LinBwd {
+  LinShape wide, deep;                     // dq and dk; dv
+  int64_t seg_q, seg_k, seg_v, part_k, part_v, bytes;
+};
+inline LinBwd lin_bwd(const pnn_linattn_desc& d) {
+  LinBwd w;
+  w.wide = lin_shape(d, d.value_width, d.key_width, 2);
+  w.deep = lin_shape(d, d.key_width, d.value_width, 1);
+  int64_t o = 0;
+  auto take = [&](int64_t bytes) {
+    const int64_t at = o;
+    o += round256(bytes);
+    return at;
+  };
+  w.seg_q = take(w.wide.bytes);
+  w.seg_k = take(w.wide.bytes);
+  w.seg_v = take(w.deep.bytes);
+  const int64_t steps = d.heads > d.kv_heads ? d.batch * d.length * d.heads * 4 : 0;
+  w.part_k = take(steps * d.key_width);
+  w.part_v = take(steps * d.value_width);
+  w.bytes = o;
+  return w;
+}
+int launch_linattn_fwd(const pnn_linattn_desc& d, const void* q, const void* k, const void* v, const float* decay,
+                       const int32_t* lengths, const float* s0, void* o, float* sT, void* ws, hipStream_t s);
+int launch_linattn_bwd(const pnn_linattn_desc& d, const void* q, const void* k, const void* v, const float* decay,
+                       const int32_t* lengths, const float* s0, const void* dout, const float* dsT, void* dq, void* dk,
+                       void* dv, float* ds0, void* ws, hipStream_t s);
+
 }  // namespace pnn

@@ -16,8 +16,9 @@ from .binding import PNN_BF16, PNN_F32, PnnError  # noqa: F401
 
 # every symbol include/pnn_seq.h declares
 EXPORTS = ["pnn_embed_fwd", "pnn_embed_workspace_size", "pnn_embed_bwd", "pnn_scan_sizes", "pnn_scan_fwd",
-           "pnn_scan_bwd", "pnn_distill_fwd_bwd"]
+           "pnn_scan_bwd", "pnn_distill_fwd_bwd", "pnn_linattn_sizes", "pnn_linattn_fwd", "pnn_linattn_bwd"]
 DISTILL_MAX_TOP = 1024
+LINATTN_MAX_WIDTH = 256
 
 _i, _i64, _f, _vp = ctypes.c_int, ctypes.c_int64, ctypes.c_float, ctypes.c_void_p
 
@@ -42,6 +43,16 @@ class DistillDesc(ctypes.Structure):
                 ("alpha", _f), ("scale", _f)]
 
 
+class HeadStride(ctypes.Structure):
+    _fields_ = [("batch", _i64), ("step", _i64), ("head", _i64)]
+
+
+class LinattnDesc(ctypes.Structure):
+    _fields_ = [("dtype", _i), ("batch", _i64), ("length", _i64), ("heads", _i64), ("kv_heads", _i64),
+                ("key_width", _i64), ("value_width", _i64)] + \
+               [(n, HeadStride) for n in ("q", "k", "v", "o", "dout", "dq", "dk", "dv")] + [("scale", _f)]
+
+
 _lib = None
 
 
@@ -60,6 +71,10 @@ def lib():
     L.pnn_scan_fwd.argtypes = [S] + [_vp] * 9
     L.pnn_scan_bwd.argtypes = [S] + [_vp] * 11
     L.pnn_distill_fwd_bwd.argtypes = [D] + [_vp] * 8
+    A = ctypes.POINTER(LinattnDesc)
+    L.pnn_linattn_sizes.argtypes = [A, szp, szp]
+    L.pnn_linattn_fwd.argtypes = [A] + [_vp] * 10
+    L.pnn_linattn_bwd.argtypes = [A] + [_vp] * 14
     _lib = L
     return L
 
@@ -130,6 +145,29 @@ def distill_desc(logits, teacher, dlogits=None, temperature=1.0, alpha=1.0, scal
     return DistillDesc(_dtype(logits), _dtype(teacher), rows, classes, top, ls, gs, ks, temperature, alpha, scale)
 
 
+def _head_stride(t, shape, dtype, what):
+    if tuple(t.shape) != shape or _dtype(t) != dtype or (shape[3] > 1 and t.stride(3) != 1):
+        raise ValueError(f"{what}: shape {tuple(t.shape)}, {t.dtype}, strides {tuple(t.stride())} do not fit "
+                         f"[batch][length][heads][width] {shape}")
+    return HeadStride(t.stride(0), t.stride(1), t.stride(2))
+
+
+def linattn_desc(q, k, v, o, dout=None, dq=None, dk=None, dv=None, scale=1.0):
+    """Queries [batch][length][heads][key width], keys and values [batch][length][kv heads][..], outputs
+    [batch][length][heads][value width], each with contiguous widths, all of one type; the gradients' (shaped like o, q,
+    k, v) may be left out for a description that only the forward uses."""
+    if q.dim() != 4 or k.dim() != 4 or v.dim() != 4:
+        raise ValueError("q, k, v: [batch][length][heads][width] expected")
+    dt = _dtype(q)
+    B, T, H, K = q.shape
+    kv, V = k.shape[2], v.shape[3]
+    qs, ks, vs, os = (B, T, H, K), (B, T, kv, K), (B, T, kv, V), (B, T, H, V)
+    st = [HeadStride(0, 0, 0) if t is None else _head_stride(t, shape, dt, n)
+          for n, t, shape in (("q", q, qs), ("k", k, ks), ("v", v, vs), ("o", o, os), ("dout", dout, os), ("dq", dq, qs),
+                              ("dk", dk, ks), ("dv", dv, vs))]
+    return LinattnDesc(dt, B, T, H, kv, K, V, *st, scale)
+
+
 # ------------------------------------------------------------------------------------------------
 # entry points (same names as the C ABI)
 # ------------------------------------------------------------------------------------------------
@@ -169,3 +207,21 @@ def pnn_scan_bwd(desc, x, gate, lengths, states, dh, dhT, dx, dgate, dh0, worksp
 def pnn_distill_fwd_bwd(desc, logits, index, teacher, labels, weight, loss, dlogits, stream):
     _check(lib().pnn_distill_fwd_bwd(desc, _ptr(logits), _ptr(index), _ptr(teacher), _ptr(labels), _ptr(weight),
                                      _ptr(loss), _ptr(dlogits), stream), "pnn_distill_fwd_bwd")
+
+
+def pnn_linattn_sizes(desc):
+    """Bytes of workspace: (forward, backward)"""
+    a, b = ctypes.c_size_t(), ctypes.c_size_t()
+    _check(lib().pnn_linattn_sizes(desc, ctypes.byref(a), ctypes.byref(b)), "pnn_linattn_sizes")
+    return a.value, b.value
+
+
+def pnn_linattn_fwd(desc, q, k, v, log_decay, lengths, s0, o, sT, workspace, stream):
+    _check(lib().pnn_linattn_fwd(desc, _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(lengths), _ptr(s0), _ptr(o),
+                                 _ptr(sT), _ptr(workspace), stream), "pnn_linattn_fwd")
+
+
+def pnn_linattn_bwd(desc, q, k, v, log_decay, lengths, s0, dout, dsT, dq, dk, dv, ds0, workspace, stream):
+    _check(lib().pnn_linattn_bwd(desc, _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(lengths), _ptr(s0), _ptr(dout),
+                                 _ptr(dsT), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(ds0), _ptr(workspace), stream),
+           "pnn_linattn_bwd")
