@@ -180,7 +180,7 @@ pnn_status pnn_linattn_sizes(const pnn_linattn_desc* d, size_t* forward, size_t*
  * (length 1, sT = s0) is the form for answering.  o may not be q, k or v.  A q, k or v that is not finite makes
  * outputs of its own step and, for k and v, of later ones not finite (infinite or NaN), none of earlier steps.
  * bf16: products that a step's output is a sum of take the weighted q k and the state rounded to bf16; the state
- * itself is a float sum of terms within 2^-16 of their values. */
+ * itself is a float sum. */
 pnn_status pnn_linattn_fwd(const pnn_linattn_desc* d, const void* q, const void* k, const void* v,
                            const float* log_decay, const int32_t* lengths, const float* s0, void* o, float* sT,
                            void* workspace, void* stream);
@@ -194,6 +194,75 @@ pnn_status pnn_linattn_fwd(const pnn_linattn_desc* d, const void* q, const void*
 pnn_status pnn_linattn_bwd(const pnn_linattn_desc* d, const void* q, const void* k, const void* v,
                            const float* log_decay, const int32_t* lengths, const float* s0, const void* dout,
                            const float* dsT, void* dq, void* dk, void* dv, float* ds0, void* workspace, void* stream);
+
+/* ---- norms before and after a block, with its gate and the residual sum ------------------------ */
+
+/* strides of a [rows][heads][width] tensor, in elements */
+typedef struct {
+  int64_t row;  /* from row to row */
+  int64_t head; /* from head to head */
+} pnn_row_stride;
+
+typedef struct {
+  int dtype;               /* pnn_dtype of x, gate, res, h, y and their gradients; weights and their gradients are float */
+  int64_t rows, heads;     /* a norm is over the width of one head of one row; 1 head: over the row */
+  int64_t width;           /* 1 .. PNN_NORM_MAX_WIDTH */
+  int post;                /* != 0: norm of the block's output x */
+  int pre;                 /* != 0: norm of the sum h, the next block's input */
+  pnn_row_stride x, gate, res, h, y;          /* forward (backward: x, gate, res) */
+  pnn_row_stride dy, dh, dx, dgate, dres;     /* backward */
+  float eps;               /* > 0 */
+  float alpha;             /* scale of the block's output in the sum */
+} pnn_norm_desc;
+
+#define PNN_NORM_MAX_WIDTH 16384
+
+/* With norm(u) = u / sqrt(mean(u^2) + eps) over the width:
+ *     a = post ? w_post norm(x) : x,   h = res + alpha a silu(gate),   y = w_pre norm(h)   (pre != 0)
+ * w_post, w_pre: float[width], the same for every head (NULL: ones).  gate, res (NULL: without), h (NULL: not wanted,
+ * with pre; may be res itself, with the same strides), y (needed if pre != 0, not looked at otherwise).  y is formed from the sum
+ * before it is rounded to h.  silu(-inf) is 0.  A row whose squares pass the float range is normed to zeros. */
+pnn_status pnn_norm_fwd(const pnn_norm_desc* d, const void* x, const float* w_post, const void* gate, const void* res,
+                        const float* w_pre, void* h, void* y, void* stream);
+
+/* Bytes of workspace for pnn_norm_bwd (needed if dw_post or dw_pre is wanted). */
+pnn_status pnn_norm_workspace_size(const pnn_norm_desc* d, size_t* bytes);
+
+/* The gradients, from dy (pre != 0) and (nullable) dh, the gradient that reaches h otherwise.  x, gate, res, w_post, w_pre
+ * as in the forward, whose h is formed again without its rounding (x is not looked at without post, pre and gate, res
+ * not without pre).  dres = dL/dres (nullable; may be dh itself, with the same strides), dx, dgate (nullable).  dw_post,
+ * dw_pre (float[width], nullable): overwritten, or added to with accumulate != 0; each sum has one order.  Without dres,
+ * dx, dgate and both weights' gradients nothing is done. */
+pnn_status pnn_norm_bwd(const pnn_norm_desc* d, const void* x, const float* w_post, const void* gate, const void* res,
+                        const float* w_pre, const void* dy, const void* dh, void* dx, void* dgate, void* dres,
+                        float* dw_post, float* dw_pre, int accumulate, void* workspace, void* stream);
+
+/* ---- clipped policy loss with a KL term -------------------------------------------------------- */
+
+typedef struct {
+  int dtype;            /* pnn_dtype of logits and dlogits */
+  int64_t rows, classes;
+  int64_t logit_stride; /* elements from row to row of logits */
+  int64_t grad_stride;  /* ... of dlogits */
+  float temperature;    /* tau > 0 */
+  float clip_low, clip_high; /* the ratio is held within 1 - clip_low .. 1 + clip_high; >= 0 */
+  float kl;             /* weight of the KL term (0: ref is not looked at) */
+  float scale;          /* factor of every gradient (1 / rows for a mean) */
+} pnn_policy_desc;
+
+/* For every row with a token a = tokens[row] >= 0, with p = softmax(logits / tau):
+ *     l = log p_a,  r = exp(l - old),  x = ref - l
+ *     loss = -min(r A, clip(r, 1 - clip_low, 1 + clip_high) A) + kl (exp(x) - 1 - x),   A = advantage
+ *     dlogits_v = scale weight c / tau ([v = a] - p_v),   c = -[r A <= clip(r) A] r A - kl (exp(x) - 1)
+ * logp (nullable): float[rows], l.  old (NULL: r = 1, with the gradient of r at 1), ref, weight (NULL: ones): float[rows].
+ * The weight is a factor of the row's gradient, not of its loss.  A row with a token below 0 (a prompt's, padding)
+ * has loss, l and gradient 0 whatever the rest of it holds; a token not below `classes` makes them NaN.
+ * loss: float[rows].  dlogits (nullable: loss and logp only) may be logits itself (with the same stride).
+ * PNN_ERR_VALUE: tau not above zero, a clip bound below zero, or tau, log2(e) / tau, a bound, kl, scale or scale / tau
+ * not finite. */
+pnn_status pnn_policy_fwd_bwd(const pnn_policy_desc* d, const void* logits, const int32_t* tokens,
+                              const float* advantage, const float* old, const float* ref, const float* weight,
+                              float* loss, float* logp, void* dlogits, void* stream);
 
 #ifdef __cplusplus
 }

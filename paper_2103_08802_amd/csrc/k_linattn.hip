@@ -19,7 +19,8 @@
 //
 // Roundings to bf16 besides the outputs' (bf16 tensors only): the weighted q k and the state, where they are operands
 // of the products with v and q; each is as large as the output's own rounding.  The state itself is fp32, and the
-// weighted values that are added to it are split into two bf16 parts (16 bits).
+// weighted values that are added to it are split into two bf16 parts (16 bits), and three (24 bits) where the caller
+// wants the state.
 #include "device_common.h"
 #include "seq_device.h"
 #include "seq_internal.h"
@@ -167,13 +168,15 @@ __device__ __forceinline__ void state_frag(Frag<float>& f, const f32x4 (&S)[KT][
 #pragma unroll
   for (int e = 0; e < 4; ++e) f.v[e] = S[kk][et][e];
 }
-// acc += a (b w): float as it is, bf16 with b w in two parts
-__device__ __forceinline__ void split(const Frag<uint16_t>& b, const float* w, Frag<uint16_t>& hi, Frag<uint16_t>& lo) {
+// b w in three parts of 8 bits
+__device__ __forceinline__ void split(const Frag<uint16_t>& b, const float* w, Frag<uint16_t> (&part)[3]) {
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const float v = (float)b.v[e] * w[e];
-    hi.v[e] = (__bf16)v;
-    lo.v[e] = (__bf16)(v - (float)hi.v[e]);
+    part[0].v[e] = (__bf16)v;
+    const float rest = v - (float)part[0].v[e];
+    part[1].v[e] = (__bf16)rest;
+    part[2].v[e] = (__bf16)(rest - (float)part[1].v[e]);
   }
 }
 __device__ __forceinline__ void finite_only(Frag<uint16_t>& f) {
@@ -264,6 +267,7 @@ __global__ __launch_bounds__(NT, 2) void linattn_kernel(Lin a) {
   if (OUT) {                                    // tiles of pt above the diagonal stay zero
     for (int x = threadIdx.x; x < C * LP; x += NT) pt[x] = (T)0;
   }
+  const bool exact = R.sT != nullptr;           // states that the caller sees
   int held = -1;                                // the length that wt is for
   // outputs of a chunk: row t's 4 ET values from column e on
   auto put = [&](int c, int t, f32x4 (&acc)[ET]) {
@@ -398,20 +402,21 @@ __global__ __launch_bounds__(NT, 2) void linattn_kernel(Lin a) {
 #pragma unroll
     for (int kb = 0; kb < C / KS; ++kb) {
       if constexpr (sizeof(T) == 2) {
-        Frag<T> hi[ET], lo[ET];
+        Frag<T> part[ET][3];
         float ws[VE];
         *(f32x4*)ws = *(const f32x4*)&wt[kb * KS + g * VE];
         *(f32x4*)(ws + 4) = *(const f32x4*)&wt[kb * KS + g * VE + 4];
 #pragma unroll
-        for (int et = 0; et < ET; ++et) split(vf[kb][et], ws, hi[et], lo[et]);
+        for (int et = 0; et < ET; ++et) split(vf[kb][et], ws, part[et]);
 #pragma unroll
         for (int dt = 0; dt < KT; ++dt) {
           Frag<T> kf;
           column_frag(kf, kt + kb * KS * LK + dt * 16, LK, i, g, 4);
 #pragma unroll
           for (int et = 0; et < ET; ++et) {
-            mma(kf, lo[et], S[dt][et]);
-            mma(kf, hi[et], S[dt][et]);
+            if (exact) mma(kf, part[et][2], S[dt][et]);
+            mma(kf, part[et][1], S[dt][et]);
+            mma(kf, part[et][0], S[dt][et]);
           }
         }
       } else {

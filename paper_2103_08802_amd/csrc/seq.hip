@@ -108,6 +108,34 @@ pnn_status linattn_in_ok(const pnn_linattn_desc* d) {
   return heads_ok(d, d->v, d->kv_heads, d->value_width, false);
 }
 
+// a [rows][heads][width] tensor; rows outside heads or heads outside rows
+pnn_status norm_rows_ok(const pnn_norm_desc* d, const pnn_row_stride& s, bool out) {
+  if (s.row < 0 || s.head < 0) return PNN_ERR_SHAPE;
+  const __int128 rows = (__int128)(d->rows - 1) * s.row, heads = (__int128)(d->heads - 1) * s.head;
+  if (rows + heads + d->width > (__int128)MAX_SPAN) return PNN_ERR_TOO_LARGE;
+  if (out) {
+    if ((d->rows > 1 && s.row < d->width) || (d->heads > 1 && s.head < d->width)) return PNN_ERR_SHAPE;
+    if (d->rows > 1 && d->heads > 1 && s.row < heads + d->width && s.head < rows + d->width) return PNN_ERR_SHAPE;
+  }
+  return PNN_OK;
+}
+
+// whether two tensors that start in one place are the same elements
+bool same(const pnn_row_stride& a, const pnn_row_stride& b, const pnn_norm_desc* d) {
+  return (d->rows <= 1 || a.row == b.row) && (d->heads <= 1 || a.head == b.head);
+}
+
+pnn_status norm_ok(const pnn_norm_desc* d) {
+  if (d == nullptr) return PNN_ERR_NULL;
+  if (!type_ok(d->dtype)) return PNN_ERR_DTYPE;
+  if (d->rows < 0 || d->heads < 1 || d->width < 1) return PNN_ERR_SHAPE;
+  // rows are counted in 32 bits, with a step of all teams (up to 2048 x 16) beyond the last
+  if (d->width > PNN_NORM_MAX_WIDTH || d->rows > (1 << 30) || d->heads > (1 << 30) || d->rows * d->heads > (1 << 30))
+    return PNN_ERR_TOO_LARGE;
+  if (!isfinite(d->eps) || !(d->eps >= 1e-37f) || !isfinite(d->alpha)) return PNN_ERR_VALUE;
+  return PNN_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -298,6 +326,106 @@ pnn_status pnn_linattn_bwd(const pnn_linattn_desc* d, const void* q, const void*
   }
   return launch_linattn_bwd(*d, q, k, v, log_decay, lengths, s0, dout, dsT, dq, dk, dv, ds0, workspace,
                             (hipStream_t)stream)
+             ? PNN_ERR_HIP
+             : PNN_OK;
+}
+
+pnn_status pnn_norm_fwd(const pnn_norm_desc* d, const void* x, const float* w_post, const void* gate, const void* res,
+                        const float* w_pre, void* h, void* y, void* stream) {
+  if (pnn_status e = norm_ok(d)) return e;
+  if (pnn_status e = norm_rows_ok(d, d->x, false)) return e;
+  if (gate != nullptr)
+    if (pnn_status e = norm_rows_ok(d, d->gate, false)) return e;
+  if (res != nullptr)
+    if (pnn_status e = norm_rows_ok(d, d->res, false)) return e;
+  if (h != nullptr)
+    if (pnn_status e = norm_rows_ok(d, d->h, true)) return e;
+  if (d->pre)
+    if (pnn_status e = norm_rows_ok(d, d->y, true)) return e;
+  if (d->rows == 0) return PNN_OK;
+  if (x == nullptr || (d->pre && y == nullptr) || (!d->pre && h == nullptr)) return PNN_ERR_NULL;
+  const int es = type_size(d->dtype);
+  if (!d->pre) y = nullptr;
+  if (!aligned(x, es) || !aligned(w_post, 4) || !aligned(gate, es) || !aligned(res, es) || !aligned(w_pre, 4) ||
+      !aligned(h, es) || !aligned(y, es))
+    return PNN_ERR_ALIGN;
+  if (h != nullptr && (h == x || h == gate || h == y)) return PNN_ERR_SHAPE;
+  if (y != nullptr && (y == x || y == gate || y == res)) return PNN_ERR_SHAPE;
+  if (h != nullptr && h == res && !same(d->h, d->res, d)) return PNN_ERR_SHAPE;
+  return launch_norm_fwd(*d, x, w_post, gate, res, w_pre, h, y, (hipStream_t)stream) ? PNN_ERR_HIP : PNN_OK;
+}
+
+pnn_status pnn_norm_workspace_size(const pnn_norm_desc* d, size_t* bytes) {
+  if (bytes == nullptr) return PNN_ERR_NULL;
+  if (pnn_status e = norm_ok(d)) return e;
+  *bytes = (size_t)norm_ws_bytes(*d);
+  return PNN_OK;
+}
+
+pnn_status pnn_norm_bwd(const pnn_norm_desc* d, const void* x, const float* w_post, const void* gate, const void* res,
+                        const float* w_pre, const void* dy, const void* dh, void* dx, void* dgate, void* dres,
+                        float* dw_post, float* dw_pre, int accumulate, void* workspace, void* stream) {
+  if (pnn_status e = norm_ok(d)) return e;
+  if (!d->pre) res = dy = nullptr, dw_pre = nullptr;
+  if (!d->post) dw_post = nullptr;
+  if (gate == nullptr) dgate = nullptr;
+  const bool needs_x = d->post || d->pre || gate != nullptr;
+  if (!needs_x) x = nullptr;
+  const struct {
+    const void* p;
+    const pnn_row_stride& s;
+    bool out;
+  } tensors[8] = {{x, d->x, false},   {gate, d->gate, false}, {res, d->res, false}, {dy, d->dy, false},
+                  {dh, d->dh, false}, {dx, d->dx, true},      {dgate, d->dgate, true}, {dres, d->dres, true}};
+  for (const auto& t : tensors)
+    if (t.p != nullptr)
+      if (pnn_status e = norm_rows_ok(d, t.s, t.out)) return e;
+  if (dx == nullptr && dgate == nullptr && dres == nullptr && dw_post == nullptr && dw_pre == nullptr) return PNN_OK;
+  if (d->rows > 0 && ((needs_x && x == nullptr) || (d->pre && dy == nullptr))) return PNN_ERR_NULL;
+  if (d->rows > 0 && (dw_post != nullptr || dw_pre != nullptr) && workspace == nullptr) return PNN_ERR_NULL;
+  const int es = type_size(d->dtype);
+  for (const auto& t : tensors)
+    if (!aligned(t.p, es)) return PNN_ERR_ALIGN;
+  if (!aligned(w_post, 4) || !aligned(w_pre, 4) || !aligned(dw_post, 4) || !aligned(dw_pre, 4) ||
+      !aligned(workspace, 256))
+    return PNN_ERR_ALIGN;
+  for (int i = 5; i < 8; ++i)
+    for (int j = 0; j < i; ++j)
+      if (tensors[i].p != nullptr && tensors[i].p == tensors[j].p && !(i == 7 && j == 4 && same(d->dres, d->dh, d)))
+        return PNN_ERR_SHAPE;
+  if (dw_post != nullptr && dw_post == dw_pre) return PNN_ERR_SHAPE;
+  return launch_norm_bwd(*d, x, w_post, gate, res, w_pre, dy, dh, dx, dgate, dres, dw_post, dw_pre, accumulate, workspace,
+                         (hipStream_t)stream)
+             ? PNN_ERR_HIP
+             : PNN_OK;
+}
+
+pnn_status pnn_policy_fwd_bwd(const pnn_policy_desc* d, const void* logits, const int32_t* tokens,
+                              const float* advantage, const float* old, const float* ref, const float* weight,
+                              float* loss, float* logp, void* dlogits, void* stream) {
+  if (d == nullptr) return PNN_ERR_NULL;
+  if (!type_ok(d->dtype)) return PNN_ERR_DTYPE;
+  if (d->rows < 0 || d->classes < 1) return PNN_ERR_SHAPE;
+  if (d->rows > (1 << 28) || d->classes > MAX_COUNT) return PNN_ERR_TOO_LARGE;
+  if (pnn_status e = rows_ok(d->rows, d->logit_stride, d->classes, false)) return e;
+  if (dlogits != nullptr)
+    if (pnn_status e = rows_ok(d->rows, d->grad_stride, d->classes, true)) return e;
+  const float tau = d->temperature;
+  if (!isfinite(tau) || !(tau > 0.0f) || !isfinite(1.44269504f / tau) || !isfinite(d->clip_low) ||
+      !isfinite(d->clip_high) || d->clip_low < 0.0f || d->clip_high < 0.0f || !isfinite(d->kl) || !isfinite(d->scale) ||
+      !isfinite(d->scale / tau))
+    return PNN_ERR_VALUE;
+  if (d->rows == 0) return PNN_OK;
+  if (logits == nullptr || tokens == nullptr || advantage == nullptr || loss == nullptr ||
+      (d->kl != 0.0f && ref == nullptr))
+    return PNN_ERR_NULL;
+  const int es = type_size(d->dtype);
+  if (!aligned(logits, es) || !aligned(dlogits, es) || !aligned(tokens, 4) || !aligned(advantage, 4) ||
+      !aligned(old, 4) || !aligned(ref, 4) || !aligned(weight, 4) || !aligned(loss, 4) || !aligned(logp, 4))
+    return PNN_ERR_ALIGN;
+  if (dlogits == logits && d->rows > 1 && d->grad_stride != d->logit_stride) return PNN_ERR_SHAPE;
+  if (loss == logp) return PNN_ERR_SHAPE;
+  return launch_policy(*d, logits, tokens, advantage, old, ref, weight, loss, logp, dlogits, (hipStream_t)stream)
              ? PNN_ERR_HIP
              : PNN_OK;
 }

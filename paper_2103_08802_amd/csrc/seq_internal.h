@@ -218,4 +218,32 @@ int launch_linattn_bwd(const pnn_linattn_desc& d, const void* q, const void* k, 
                        const int32_t* lengths, const float* s0, const void* dout, const float* dsT, void* dq, void* dk,
                        void* dv, float* ds0, void* ws, hipStream_t s);
 
+// ---- norms ----
+// How rows run: lanes and 16-byte pieces a lane of one, workgroups of the forward and the backward
+struct NormShape {
+  int lanes, pieces, forward, backward;
+};
+inline NormShape norm_shape(const pnn_norm_desc& d) {
+  NormShape p;
+  const int64_t n = cdiv64(d.width, d.dtype == PNN_F32 ? 4 : 8), rows = d.rows * d.heads;
+  p.lanes = n <= 32 ? 16 : n <= 128 ? 64 : n <= 512 ? 256 : 1024;
+  p.pieces = n <= p.lanes ? 1 : n <= 2 * p.lanes ? 2 : 4;
+  const int64_t teams = p.lanes < 256 ? 256 / p.lanes : 1, wgs = cdiv64(rows, teams);
+  const int64_t most_f = p.lanes == 1024 ? 512 : 2048, most_b = p.lanes == 1024 ? 256 : 1024;
+  p.forward = (int)(wgs < most_f ? wgs : most_f);
+  p.backward = (int)(wgs < most_b ? wgs : most_b);
+  return p;
+}
+inline int64_t norm_ws_bytes(const pnn_norm_desc& d) { return (int64_t)norm_shape(d).backward * 2 * d.width * 4; }
+int launch_norm_fwd(const pnn_norm_desc& d, const void* x, const float* w_post, const void* gate, const void* res,
+                    const float* w_pre, void* h, void* y, hipStream_t s);
+int launch_norm_bwd(const pnn_norm_desc& d, const void* x, const float* w_post, const void* gate, const void* res,
+                    const float* w_pre, const void* dy, const void* dh, void* dx, void* dgate, void* dres,
+                    float* dw_post, float* dw_pre, int accumulate, void* ws, hipStream_t s);
+
+// ---- policy loss ----
+int launch_policy(const pnn_policy_desc& d, const void* logits, const int32_t* tokens, const float* advantage,
+                  const float* old, const float* ref, const float* weight, float* loss, float* logp, void* dlogits,
+                  hipStream_t s);
+
 }  // namespace pnn

@@ -1,10 +1,10 @@
 """Thin ctypes binding of libpnn's sequence operators (``include/pnn_seq.h``): token embedding, gated linear
-recurrence and distillation loss.
+recurrence, linear attention, norms, distillation and policy loss.
 
 Every ``pnn_*`` function has the name of the C entry point it calls and takes a description, device
 pointers as Python ints or objects with ``data_ptr()`` (None: NULL) and a stream.  ``embed_desc``,
-``scan_desc`` and ``distill_desc`` fill the descriptions from tensors; fill one once and use it for every
-call on tensors of the same types, shapes and strides.  As in ``binding``, nothing falls back to anything
+``scan_desc``, ``distill_desc``, ``linattn_desc``, ``norm_desc`` and ``policy_desc`` fill the descriptions from
+tensors; fill one once and use it for every call on tensors of the same types, shapes and strides.  As in ``binding``, nothing falls back to anything
 else: a refused call raises ``PnnError``.
 """
 from __future__ import annotations
@@ -16,9 +16,11 @@ from .binding import PNN_BF16, PNN_F32, PnnError  # noqa: F401
 
 # every symbol include/pnn_seq.h declares
 EXPORTS = ["pnn_embed_fwd", "pnn_embed_workspace_size", "pnn_embed_bwd", "pnn_scan_sizes", "pnn_scan_fwd",
-           "pnn_scan_bwd", "pnn_distill_fwd_bwd", "pnn_linattn_sizes", "pnn_linattn_fwd", "pnn_linattn_bwd"]
+           "pnn_scan_bwd", "pnn_distill_fwd_bwd", "pnn_linattn_sizes", "pnn_linattn_fwd", "pnn_linattn_bwd",
+           "pnn_norm_fwd", "pnn_norm_workspace_size", "pnn_norm_bwd", "pnn_policy_fwd_bwd"]
 DISTILL_MAX_TOP = 1024
 LINATTN_MAX_WIDTH = 256
+NORM_MAX_WIDTH = 16384
 
 _i, _i64, _f, _vp = ctypes.c_int, ctypes.c_int64, ctypes.c_float, ctypes.c_void_p
 
@@ -53,6 +55,21 @@ class LinattnDesc(ctypes.Structure):
                [(n, HeadStride) for n in ("q", "k", "v", "o", "dout", "dq", "dk", "dv")] + [("scale", _f)]
 
 
+class RowStride(ctypes.Structure):
+    _fields_ = [("row", _i64), ("head", _i64)]
+
+
+class NormDesc(ctypes.Structure):
+    _fields_ = [("dtype", _i), ("rows", _i64), ("heads", _i64), ("width", _i64), ("post", _i), ("pre", _i)] + \
+               [(n, RowStride) for n in ("x", "gate", "res", "h", "y", "dy", "dh", "dx", "dgate", "dres")] + \
+               [("eps", _f), ("alpha", _f)]
+
+
+class PolicyDesc(ctypes.Structure):
+    _fields_ = [("dtype", _i), ("rows", _i64), ("classes", _i64), ("logit_stride", _i64), ("grad_stride", _i64),
+                ("temperature", _f), ("clip_low", _f), ("clip_high", _f), ("kl", _f), ("scale", _f)]
+
+
 _lib = None
 
 
@@ -75,6 +92,11 @@ def lib():
     L.pnn_linattn_sizes.argtypes = [A, szp, szp]
     L.pnn_linattn_fwd.argtypes = [A] + [_vp] * 10
     L.pnn_linattn_bwd.argtypes = [A] + [_vp] * 14
+    N = ctypes.POINTER(NormDesc)
+    L.pnn_norm_fwd.argtypes = [N] + [_vp] * 8
+    L.pnn_norm_workspace_size.argtypes = [N, szp]
+    L.pnn_norm_bwd.argtypes = [N] + [_vp] * 12 + [_i, _vp, _vp]
+    L.pnn_policy_fwd_bwd.argtypes = [ctypes.POINTER(PolicyDesc)] + [_vp] * 10
     _lib = L
     return L
 
@@ -168,6 +190,37 @@ def linattn_desc(q, k, v, o, dout=None, dq=None, dk=None, dv=None, scale=1.0):
     return LinattnDesc(dt, B, T, H, kv, K, V, *st, scale)
 
 
+def norm_desc(x, gate=None, res=None, h=None, y=None, dy=None, dh=None, dx=None, dgate=None, dres=None, post=False,
+              pre=False, eps=1e-5, alpha=1.0):
+    """Tensors [rows][heads][width], or [rows][width] for one head, with contiguous widths, all of x's type and shape; those
+    that no call uses may be left out.  ``post``: norm of x, ``pre``: norm of h."""
+    if x.dim() not in (2, 3):
+        raise ValueError(f"x: [rows][heads][width] or [rows][width] expected, not {tuple(x.shape)}")
+    dt, shape = _dtype(x), tuple(x.shape)
+    st = []
+    for n, t in (("x", x), ("gate", gate), ("res", res), ("h", h), ("y", y), ("dy", dy), ("dh", dh), ("dx", dx),
+                 ("dgate", dgate), ("dres", dres)):
+        if t is None:
+            st.append(RowStride(0, 0))
+            continue
+        if tuple(t.shape) != shape or _dtype(t) != dt or (shape[-1] > 1 and t.stride(-1) != 1):
+            raise ValueError(f"{n}: shape {tuple(t.shape)}, {t.dtype}, strides {tuple(t.stride())} do not fit")
+        st.append(RowStride(t.stride(0), t.stride(1) if len(shape) == 3 else shape[-1]))
+    return NormDesc(dt, shape[0], shape[1] if len(shape) == 3 else 1, shape[-1], int(bool(post)), int(bool(pre)), *st,
+                    eps, alpha)
+
+
+def policy_desc(logits, dlogits=None, temperature=1.0, clip_low=0.2, clip_high=0.2, kl=0.0, scale=1.0):
+    """Logits [rows][classes] and, unless only the loss and the log probabilities are wanted, dlogits like logits."""
+    rows, classes, ls = _rows(logits, "logits")
+    gs = ls
+    if dlogits is not None:
+        gn, gw, gs = _rows(dlogits, "dlogits")
+        if (gn, gw) != (rows, classes) or dlogits.dtype != logits.dtype:
+            raise ValueError("dlogits and logits differ in shape or type")
+    return PolicyDesc(_dtype(logits), rows, classes, ls, gs, temperature, clip_low, clip_high, kl, scale)
+
+
 # ------------------------------------------------------------------------------------------------
 # entry points (same names as the C ABI)
 # ------------------------------------------------------------------------------------------------
@@ -225,3 +278,25 @@ def pnn_linattn_bwd(desc, q, k, v, log_decay, lengths, s0, dout, dsT, dq, dk, dv
     _check(lib().pnn_linattn_bwd(desc, _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(lengths), _ptr(s0), _ptr(dout),
                                  _ptr(dsT), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(ds0), _ptr(workspace), stream),
            "pnn_linattn_bwd")
+
+
+def pnn_norm_fwd(desc, x, w_post, gate, res, w_pre, h, y, stream):
+    _check(lib().pnn_norm_fwd(desc, _ptr(x), _ptr(w_post), _ptr(gate), _ptr(res), _ptr(w_pre), _ptr(h), _ptr(y), stream),
+           "pnn_norm_fwd")
+
+
+def pnn_norm_workspace_size(desc):
+    v = ctypes.c_size_t()
+    _check(lib().pnn_norm_workspace_size(desc, ctypes.byref(v)), "pnn_norm_workspace_size")
+    return v.value
+
+
+def pnn_norm_bwd(desc, x, w_post, gate, res, w_pre, dy, dh, dx, dgate, dres, dw_post, dw_pre, accumulate, workspace, stream):
+    _check(lib().pnn_norm_bwd(desc, _ptr(x), _ptr(w_post), _ptr(gate), _ptr(res), _ptr(w_pre), _ptr(dy), _ptr(dh), _ptr(dx),
+                              _ptr(dgate), _ptr(dres), _ptr(dw_post), _ptr(dw_pre), int(bool(accumulate)),
+                              _ptr(workspace), stream), "pnn_norm_bwd")
+
+
+def pnn_policy_fwd_bwd(desc, logits, tokens, advantage, old, ref, weight, loss, logp, dlogits, stream):
+    _check(lib().pnn_policy_fwd_bwd(desc, _ptr(logits), _ptr(tokens), _ptr(advantage), _ptr(old), _ptr(ref),
+                                    _ptr(weight), _ptr(loss), _ptr(logp), _ptr(dlogits), stream), "pnn_policy_fwd_bwd")
