@@ -6,8 +6,8 @@
 //   S  <- lambda^len S + sum_j k_j (lambda^(len - 1 - j) v_j)^T,
 // four products on the matrix units.  A workgroup of four waves takes 64 ET value columns of a head through the
 // chunks; a wave holds the state of its 16 ET columns in registers, in the layout that the products leave it in and
-// that they take it in (rows d of a state column are the summation index of q S, so the column's registers are an
-// operand as they stand, with the summation index permuted).  q k is formed once a workgroup and goes through LDS.
+// that they take it in (a state column's rows are the summation index of q S, so its registers are an operand as they
+// stand).  q k is formed once a workgroup and goes through LDS.
 //
 // The backward is the same sum three times:
 //   dq: queries do, keys v, values k, from the transposed state;
@@ -29,7 +29,8 @@ namespace pnn {
 
 namespace {
 
-constexpr int NT = 256;                     // threads: four waves
+constexpr int C = LIN_CHUNK;
+constexpr int NT = 256;                     // threads of the small kernels
 constexpr int AHEAD = 8;                    // state rows a lane of the single step has in flight
 constexpr float LOG2E = 1.44269504f;
 
@@ -46,7 +47,7 @@ struct Role {
   int o_float;                              // o is fp32 whatever the type
   int shift;                                // 1: backwards in time
   float intra, inter, update;               // factors of the three sums
-  int blocks, first;                        // value blocks; first workgroup of the role in the launch
+  int blocks;                               // workgroups a head's value columns are dealt to
 };
 
 struct Lin {
@@ -55,6 +56,8 @@ struct Lin {
   const int32_t* lengths;
   int roles, batch, heads, length;
   int nseg, seg_chunks;                     // segments and chunks of one
+  int most;                                 // blocks of the role with the most
+  int items;                                // batch x heads x segments
 };
 
 // log2 of a head's decay; NaN for what is none
@@ -71,56 +74,89 @@ __device__ __forceinline__ int steps_of(const int32_t* lengths, int b, int lengt
   const int n = lengths[b];
   return n < 0 ? 0 : n < length ? n : length;
 }
-__device__ __forceinline__ bool lost(float v) { return !(fabsf(v) < INFINITY); }
 
-// rows of a chunk in registers, 16 bytes a lane and row piece
-template <typename T, int C, int W>
+// Rows of a chunk on their way through registers, 16 bytes a lane and row piece.  The piece that the row's end cuts is
+// loaded and stored so that it ends there, over elements of the piece before it.  Rows shorter than a piece are copied
+// when they are stored.  What is behind a row's end in LDS stays as clear() left it.
+template <typename T, int NT, int W, int PAD>
 struct Stage {
-  static constexpr int VE = St<T>::VE, PR = W / VE, N = C * PR / NT, LD = W + VE;   // LD: a row in LDS, 16 bytes longer
+  static constexpr int VE = St<T>::VE, PR = W / VE, N = (C * PR + NT - 1) / NT, LD = W + PAD * VE;   // LD: elements of a row in LDS
+  static constexpr int ROWS = NT / PR;      // rows that the lanes' first pieces are of
+  static_assert(N == 1 || N * NT == C * PR, "whole pieces");
+  const T* p;                               // the lane's first piece of the next chunk; short rows: the chunk
+  int64_t step;
+  int col, width, now;                      // the lane's column, -1: none; rows of the sequence in the chunk held
+  int row0;                                 // the lane's first row
   uint4 r[N];
 
-  // row i is step `base + i`, of n; backwards in time step n - 1 - (base + i)
-  __device__ __forceinline__ void load(const T* p, int64_t step, int width, int base, int n, int shift) {
-    const int col = (threadIdx.x % PR) * VE;
+  // the sequence's row 0 (its last one backwards in time), elements from row to row, elements of a row
+  __device__ __forceinline__ void begin(const T* first, int64_t step_, int width_, int64_t row) {
+    step = step_;
+    width = width_;
+    col = (threadIdx.x % PR) * VE;
+    if (col >= width || width < VE || (int)threadIdx.x >= C * PR) col = -1;
+    else if (col + VE > width) col = width - VE;
+    p = first + row * step;
+    if (width >= VE && col >= 0) p += (int)(threadIdx.x / PR) * step + col;
+    row0 = col < 0 ? 0 : threadIdx.x / PR;
+  }
+  static __device__ __forceinline__ void clear(T* lds) {
+    for (int x = threadIdx.x; x < C * LD; x += NT) lds[x] = (T)0;
+  }
+  // The next chunk, of which `len` > 0 rows belong to the sequence.  Nothing here depends on the lane but addresses (a
+  // load under a condition waits for the one before it): lanes that store nothing load the chunk's first column, and those of rows behind the sequence's end its last row.
+  __device__ __forceinline__ void load(int len) {
+    now = len;
+    if (width < VE) return;
+    if (len >= C) {
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-      const int i = base + threadIdx.x / PR + j * (NT / PR);
-      r[j] = make_uint4(0, 0, 0, 0);
-      if (i >= n || col >= width) continue;
-      const T* s = p + (int64_t)(shift ? n - 1 - i : i) * step + col;
-      if (col + VE <= width) {
-        const typename Piece<T>::Vec u = *(const typename Piece<T>::Mem*)s;
-        r[j] = __builtin_bit_cast(uint4, u);
-      } else {
-        T e[VE];
+      for (int j = 0; j < N; ++j) r[j] = piece(p + j * ROWS * step);
+    } else {
 #pragma unroll
-        for (int x = 0; x < VE; ++x) e[x] = col + x < width ? s[x] : (T)0;
-        __builtin_memcpy(&r[j], e, 16);
+      for (int j = 0; j < N; ++j) {
+        const int last = len - 1 - row0;
+        r[j] = piece(p + (j * ROWS < last ? j * ROWS : last) * step);
       }
     }
   }
-  __device__ __forceinline__ void store(T* lds) const {
-    const int col = (threadIdx.x % PR) * VE;
-#pragma unroll
-    for (int j = 0; j < N; ++j) *(uint4*)(lds + (threadIdx.x / PR + j * (NT / PR)) * LD + col) = r[j];
+  static __device__ __forceinline__ uint4 piece(const T* s) {
+    return __builtin_bit_cast(uint4, *(const typename Piece<T>::Mem*)s);
   }
-  // whether a value is infinite or NaN
+  __device__ __forceinline__ void store(T* lds) {
+    if (width >= VE) {
+      if (now < C) {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+          if (row0 + j * ROWS >= now) r[j] = make_uint4(0, 0, 0, 0);
+      }
+      if (col >= 0) {
+        typedef typename Piece<T>::Mem Mem;
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+          *(Mem*)(lds + (row0 + j * ROWS) * LD + col) = __builtin_bit_cast(typename Piece<T>::Vec, r[j]);
+      }
+    } else {
+      for (int x = threadIdx.x; x < C * VE; x += NT) {
+        const int row = x / VE, c = x % VE;
+        if (c < width) lds[row * LD + c] = row < now ? p[row * step + c] : (T)0;
+      }
+    }
+    p += C * step;
+  }
+  // whether a value is infinite or NaN (short rows: not looked at)
   __device__ __forceinline__ bool lost() const {
-    uint32_t m = 0;
+    if (width < VE) return true;
+    if (col < 0) return false;
+    typedef typename std::conditional<sizeof(T) == 2, uint16_t, uint32_t>::type U;
+    typedef U Bits __attribute__((ext_vector_type(16 / sizeof(T))));
+    constexpr U TOP = (U)(sizeof(T) == 2 ? 0x7f80u : 0x7f800000u), ALL = (U)(sizeof(T) == 2 ? 0x7fffu : 0x7fffffffu);
+    Bits m = {};
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-      const uint32_t w[4] = {r[j].x, r[j].y, r[j].z, r[j].w};
+    for (int j = 0; j < N; ++j) m = __builtin_elementwise_max(m, __builtin_bit_cast(Bits, r[j]) & ALL);
+    bool any = false;
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        if constexpr (sizeof(T) == 2) {
-          m |= (w[x] & 0x7f80u) == 0x7f80u;
-          m |= (w[x] & 0x7f800000u) == 0x7f800000u;
-        } else {
-          m |= (w[x] & 0x7f800000u) == 0x7f800000u;
-        }
-      }
-    }
-    return m != 0;
+    for (int x = 0; x < VE; ++x) any |= m[x] >= TOP;
+    return any;
   }
 };
 
@@ -130,14 +166,6 @@ __device__ __forceinline__ Frag<T> row_frag(const T* p) {
   Frag<T> f;
   f.from_raw(*(const uint4*)p);
   return f;
-}
-// the same with the summation index in the order of state_frag
-__device__ __forceinline__ void query_frag(Frag<uint16_t>& f, const uint16_t* row, int kk, int g) {
-  const uint2 a = *(const uint2*)(row + kk * 32 + 4 * g), b = *(const uint2*)(row + kk * 32 + 16 + 4 * g);
-  f.from_raw(make_uint4(a.x, a.y, b.x, b.y));
-}
-__device__ __forceinline__ void query_frag(Frag<float>& f, const float* row, int kk, int g) {
-  f.from_raw(*(const uint4*)(row + kk * 16 + 4 * g));
 }
 // operand from the columns of a matrix in LDS, summation index down the column: lane (i, g) takes column
 // (i >> 2) spread + (i & 3) of `m` and VE rows from VE g on
@@ -154,41 +182,58 @@ __device__ __forceinline__ void column_frag(Frag<float>& f, const float* m, int 
 #pragma unroll
   for (int e = 0; e < 4; ++e) f.v[e] = p[e * ld];
 }
-// the state's columns as an operand: summation index d = 32 kk + 4 g + (0 .. 3) and 16 more (float: 16 kk + 4 g + ..)
-template <int KT, int ET>
-__device__ __forceinline__ void state_frag(Frag<uint16_t>& f, const f32x4 (&S)[KT][ET], int kk, int et) {
+// A state tile's rows: row 4 g + r of tile dt is d = state_row(dt, g) + r.  bf16: chosen so that the lane's rows of two
+// tiles are eight in a row, which is an operand's summation order; float: four of one tile are.
+template <typename T>
+__device__ __forceinline__ int state_row(int dt, int g) {
+  return sizeof(T) == 2 ? 32 * (dt >> 1) + 8 * g + 4 * (dt & 1) : 16 * dt + 4 * g;
+}
+// the keys' columns that go with them
+template <typename T>
+__device__ __forceinline__ void key_frag(Frag<T>& f, const T* m, int ld, int dt, int i, int g) {
+  if constexpr (sizeof(T) == 2) column_frag(f, m + 32 * (dt >> 1) + 4 * (dt & 1), ld, i, g, 8);
+  else column_frag(f, m + 16 * dt, ld, i, g, 4);
+}
+// the state's columns as an operand of step kk
+template <int KT>
+__device__ __forceinline__ void state_frag(Frag<uint16_t>& f, const f32x4 (&S)[KT], int kk) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    f.v[e] = (__bf16)S[2 * kk][et][e];
-    f.v[4 + e] = (__bf16)S[2 * kk + 1][et][e];
+    f.v[e] = (__bf16)S[2 * kk][e];
+    f.v[4 + e] = (__bf16)S[2 * kk + 1][e];
   }
 }
-template <int KT, int ET>
-__device__ __forceinline__ void state_frag(Frag<float>& f, const f32x4 (&S)[KT][ET], int kk, int et) {
+template <int KT>
+__device__ __forceinline__ void state_frag(Frag<float>& f, const f32x4 (&S)[KT], int kk) {
 #pragma unroll
-  for (int e = 0; e < 4; ++e) f.v[e] = S[kk][et][e];
+  for (int e = 0; e < 4; ++e) f.v[e] = S[kk][e];
 }
-// b w in three parts of 8 bits
-__device__ __forceinline__ void split(const Frag<uint16_t>& b, const float* w, Frag<uint16_t> (&part)[3]) {
+// v w in parts of 8 bits: the two largest, and with them what is left
+__device__ __forceinline__ void split(const Frag<uint16_t>& v, const float* w, Frag<uint16_t> (&part)[2], float* rest) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  const uint4 u = __builtin_bit_cast(uint4, v.v);
+  const uint32_t in[4] = {u.x, u.y, u.z, u.w};
+  uint32_t out[2][4];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const float v = (float)b.v[e] * w[e];
-    part[0].v[e] = (__bf16)v;
-    const float rest = v - (float)part[0].v[e];
-    part[1].v[e] = (__bf16)rest;
-    part[2].v[e] = (__bf16)(rest - (float)part[1].v[e]);
+  for (int e = 0; e < 4; ++e) {
+    float a = __uint_as_float(in[e] << 16) * w[2 * e], b = __uint_as_float(in[e] & 0xffff0000u) * w[2 * e + 1];
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {
+      const uint32_t c = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{a, b}), bf16x2));
+      out[p][e] = c;
+      a -= __uint_as_float(c << 16);
+      b -= __uint_as_float(c & 0xffff0000u);
+    }
+    rest[2 * e] = a;
+    rest[2 * e + 1] = b;
   }
-}
-__device__ __forceinline__ void finite_only(Frag<uint16_t>& f) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e)
-    if (lost((float)f.v[e])) f.v[e] = (__bf16)0.0f;
+  for (int p = 0; p < 2; ++p) part[p].from_raw(make_uint4(out[p][0], out[p][1], out[p][2], out[p][3]));
 }
-__device__ __forceinline__ void finite_only(Frag<float>& f) {
-#pragma unroll
-  for (int e = 0; e < 4; ++e)
-    if (lost(f.v[e])) f.v[e] = 0.0f;
-}
+
+// nothing moves over this: without it the compiler has the next products' operands in registers, and spills
+__device__ __forceinline__ void phase_end() { __builtin_amdgcn_sched_barrier(0); }
 
 template <typename T>
 __device__ __forceinline__ void put4(T* p, f32x4 v) {      // aligned
@@ -202,108 +247,136 @@ __device__ __forceinline__ void put4(T* p, f32x4 v) {      // aligned
   }
 }
 
-// KD: inner width, padded; a workgroup has 64 ET value columns; OUT: outputs, not the state alone
-template <typename T, int KD, int ET, int C, bool OUT>
-__global__ __launch_bounds__(NT, 2) void linattn_kernel(Lin a) {
-  constexpr int VE = St<T>::VE, KS = 4 * VE, KT = KD / 16, CT = C / 16, EB = 64 * ET;
-  typedef Stage<T, C, KD> SK;
-  typedef Stage<T, C, EB> SV;
-  constexpr int LK = SK::LD, LV = SV::LD, LP = C + VE;
+// four neighbouring values, rounded, to any alignment
+template <typename T>
+__device__ __forceinline__ void put_any(T* p, f32x4 v) {
+  typedef T V __attribute__((ext_vector_type(4)));
+  typedef V VM __attribute__((aligned(sizeof(T))));
+  V u;
+#pragma unroll
+  for (int x = 0; x < 4; ++x) {
+    if constexpr (sizeof(T) == 4) u[x] = v[x];
+    else u[x] = f2bf(v[x]);
+  }
+  *(VM*)p = u;
+}
+
+// waves that a SIMD is to hold, as far as registers and LDS allow
+constexpr int lin_occupancy(int size, int pad, int waves) {
+  if (size == 4) return pad == 64 ? (waves == 4 ? 3 : 4) : pad == 128 ? 2 : waves == 4 ? 1 : 2;
+  return pad == 64 ? 4 : pad == 128 ? (waves == 4 ? 3 : 4) : 2;
+}
+
+// KD: inner width, padded; NW waves of 16 value columns each; OUT: outputs, not the state alone.
+// Two workgroups of eight waves a CU: what a wave waits for (LDS, barriers) is two thirds of its time.
+template <typename T, int KD, int NW, bool OUT>
+__global__ __launch_bounds__(64 * NW, lin_occupancy(sizeof(T), KD, NW)) void linattn_kernel(Lin a) {
+  constexpr int NT = 64 * NW, VE = St<T>::VE, KS = 4 * VE, KT = KD / 16, CT = C / 16, EB = 16 * NW;
+  constexpr int TILES = CT * (CT + 1) / 2;      // tiles of pt on or below the diagonal, one a wave
+  static_assert(CT == 2 && TILES <= NW, "tiles of pt");
+  // Rows in LDS are longer than they need be by as many 16 bytes as keep the lanes of a read in different banks: 1 where
+  // rows are read along (queries), 4 where columns are (values), 6 where both are (keys).
+  typedef Stage<T, NT, KD, 1> SQ;
+  typedef Stage<T, NT, KD, 6> SK;
+  typedef Stage<T, NT, EB, 4> SV;
+  constexpr int LQ = SQ::LD, LK = SK::LD, LV = SV::LD, LP = C + VE;
   __shared__ __attribute__((aligned(16))) T kt[C * LK];
   __shared__ __attribute__((aligned(16))) T vt[C * LV];
-  __shared__ __attribute__((aligned(16))) T qt[OUT ? C * LK : 1];
+  __shared__ __attribute__((aligned(16))) T qt[OUT ? C * LQ : 1];
   __shared__ __attribute__((aligned(16))) T pt[OUT ? C * LP : 1];
-  __shared__ __attribute__((aligned(16))) float wt[C];
+  __shared__ __attribute__((aligned(16))) float wt[C], near[OUT ? C : 1], from[OUT ? C : 1];
   __shared__ int bad;
-  int z = 0;
-  while (z + 1 < a.roles && (int)blockIdx.x >= a.role[z + 1].first) ++z;
-  const Role& R = a.role[z];
-  int at = blockIdx.x - R.first;
-  const int block = at % R.blocks;
-  at /= R.blocks;
-  const int seg = at % a.nseg, bh = at / a.nseg;
+  // workgroups eight apart run on one XCD and share its L2: the roles and value blocks of a head and segment, which read
+  // the same tensors
+  const int inside = blockIdx.x / 8 % (a.roles * a.most), item = blockIdx.x / 8 / (a.roles * a.most) * 8 + blockIdx.x % 8;
+  const Role& R = a.role[inside / a.most];
+  const int block = inside % a.most;
+  if (item >= a.items || block >= R.blocks) return;
+  const int seg = item % a.nseg, bh = item / a.nseg;
   const int b = bh / a.heads, h = bh % a.heads;
-  const int w = threadIdx.x / 64, lane = threadIdx.x & 63, i = lane & 15, g = lane >> 4;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63;
   const int n = steps_of(a.lengths, b, a.length);
   const float l2 = log2_decay(a.decay, h);
-  const T* q = (const T*)R.q + b * R.qs.batch + (h / R.q_group) * R.qs.head;
-  const T* k = (const T*)R.k + b * R.ks.batch + (h / R.k_group) * R.ks.head;
-  const T* v = (const T*)R.v + b * R.vs.batch + (h / R.v_group) * R.vs.head + block * EB;
-  const int e0 = block * EB + w * 16 * ET;             // the wave's first value column
-  const int vwidth = R.value - block * EB;
-  // state: S[dt][et][r] is row d = 16 dt + 4 g + r of column e0 + 4 ET (i >> 2) + 4 et + (i & 3)
-  const int se = e0 + 4 * ET * (i >> 2) + (i & 3);
-  f32x4 S[KT][ET];
+  const int e0 = block * EB + w * 16;                  // the wave's first value column
+  const bool mine = e0 < R.value;
+  // state: S[dt][r] is row state_row(dt, lane >> 4) + r of column e0 + (lane & 15)
+  f32x4 S[KT];
   const int64_t state = (int64_t)bh * R.inner * R.value;
   float* const segment = R.seg == nullptr ? nullptr
-      : R.seg + ((((int64_t)bh * a.nseg + seg) * R.blocks + block) * 4 + w) * (KT * ET * 256) + lane * 4;
+      : R.seg + ((((int64_t)bh * a.nseg + seg) * R.blocks + block) * NW + w) * (KT * 256) + lane * 4;
 #pragma unroll
-  for (int dt = 0; dt < KT; ++dt)
+  for (int dt = 0; dt < KT; ++dt) {
+    f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (OUT && segment != nullptr) {
+      s = *(const f32x4*)(segment + dt * 256);
+    } else if (OUT && R.s0 != nullptr) {
 #pragma unroll
-    for (int et = 0; et < ET; ++et) {
-      f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
-      if (OUT && segment != nullptr) {
-        s = *(const f32x4*)(segment + (dt * ET + et) * 256);
-      } else if (OUT && R.s0 != nullptr) {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int d = 16 * dt + 4 * g + r, e = se + 4 * et;
-          if (d < R.inner && e < R.value) s[r] = R.s0[state + d * R.s_inner + e * R.s_value];
-        }
+      for (int r = 0; r < 4; ++r) {
+        const int d = state_row<T>(dt, lane >> 4) + r, e = e0 + (lane & 15);
+        if (d < R.inner && e < R.value) s[r] = R.s0[state + d * R.s_inner + e * R.s_value];
       }
-      S[dt][et] = s;
     }
+    S[dt] = s;
+  }
   const int chunks = (a.length + C - 1) / C;
   const int c0 = seg * a.seg_chunks, c1 = c0 + a.seg_chunks < chunks ? c0 + a.seg_chunks : chunks;
   const int live = (n + C - 1) / C < c1 ? (n + C - 1) / C : c1;       // chunks with steps
-  SK rq, rk;
+  SQ rq;
+  SK rk;
   SV rv;
+  {
+    // backwards in time row 0 is step n - 1 and the rows go down
+    const int64_t row = (int64_t)c0 * C;
+    auto first = [&](const void* base, const pnn_head_stride& s, int group) {
+      return (const T*)base + (b * s.batch + (h / group) * s.head + (R.shift && n > 0 ? (n - 1) * s.step : 0));
+    };
+    auto step = [&](const pnn_head_stride& s) { return R.shift ? -s.step : s.step; };
+    if (OUT) rq.begin(first(R.q, R.qs, R.q_group), step(R.qs), R.inner, row);
+    rk.begin(first(R.k, R.ks, R.k_group), step(R.ks), R.inner, row);
+    rv.begin(first(R.v, R.vs, R.v_group) + block * EB, step(R.vs), R.value - block * EB, row);
+  }
   auto load = [&](int c) {
-    if (OUT) rq.load(q, R.qs.step, R.inner, c * C, n, R.shift);
-    rk.load(k, R.ks.step, R.inner, c * C, n, R.shift);
-    rv.load(v, R.vs.step, vwidth, c * C, n, R.shift);
+    const int len = n - c * C;
+    if (OUT) rq.load(len);
+    rk.load(len);
+    rv.load(len);
   };
   if (c0 < live) load(c0);
-  if (OUT) {                                    // tiles of pt above the diagonal stay zero
+  if (OUT) SQ::clear(qt);
+  SK::clear(kt);
+  SV::clear(vt);
+  if constexpr (OUT) {                          // tiles of pt above the diagonal stay zero
     for (int x = threadIdx.x; x < C * LP; x += NT) pt[x] = (T)0;
+    for (int x = threadIdx.x; x < C; x += NT) {
+      near[C - 1 - x] = R.intra * power(l2, x);
+      from[x] = R.inter * power(l2, x + 1 - R.shift);
+    }
   }
   const bool exact = R.sT != nullptr;           // states that the caller sees
-  int held = -1;                                // the length that wt is for
-  // outputs of a chunk: row t's 4 ET values from column e on
-  auto put = [&](int c, int t, f32x4 (&acc)[ET]) {
-    const int gi = c * C + t;
-    if (gi >= a.length) return;
-    const int step = R.shift && gi < n ? n - 1 - gi : gi;
-    const int e = e0 + 4 * ET * g;
-    if (gi >= n) {
-#pragma unroll
-      for (int et = 0; et < ET; ++et) acc[et] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    }
-    const int64_t o = b * R.os.batch + step * R.os.step + h * R.os.head + e;
-    if (R.o_float) {
-#pragma unroll
-      for (int x = 0; x < 4 * ET; ++x)
-        if (e + x < R.value) ((float*)R.o)[o + x] = acc[x / 4][x % 4];
-      return;
-    }
-    constexpr int PC = 4 * ET;
-    if (e + PC <= R.value) {
-      typedef T V __attribute__((ext_vector_type(PC)));
-      typedef V VM __attribute__((aligned(sizeof(T))));
-      V u;
-#pragma unroll
-      for (int x = 0; x < PC; ++x) {
-        if constexpr (sizeof(T) == 4) u[x] = acc[x / 4][x % 4];
-        else u[x] = f2bf(acc[x / 4][x % 4]);
-      }
-      *(VM*)((T*)R.o + o) = u;
+  int held = -1;                                // the length that wt and gone are for
+  float gone = 0.0f;
+  // outputs: four values of a step, from the lane's column on
+  const int e = e0 + 4 * (lane >> 4);
+  const int64_t start = b * R.os.batch + h * R.os.head + e;
+  auto put = [&](int64_t o, f32x4 v) {
+    if (e + 4 <= R.value) {
+      if (R.o_float) put_any((float*)R.o + o, v);
+      else put_any((T*)R.o + o, v);
     } else {
 #pragma unroll
-      for (int x = 0; x < PC; ++x)
-        if (e + x < R.value) St<T>::st(R.o, o + x, acc[x / 4][x % 4]);
+      for (int x = 0; x < 4; ++x) {
+        if (e + x >= R.value) continue;
+        if (R.o_float) ((float*)R.o)[o + x] = v[x];
+        else St<T>::st(R.o, o + x, v[x]);
+      }
     }
   };
+  const int64_t ostep = R.shift ? -R.os.step : R.os.step;
+  const int64_t orow = start + (R.shift ? (n - 1) * R.os.step : 0) + (lane & 15) * ostep;
   for (int c = c0; c < live; ++c) {
+    // addresses in LDS formed anew each time: kept, they cost 60 registers
+    int i = lane & 15, g = lane >> 4;
+    asm volatile("" : "+v"(i), "+v"(g));
     const int len = n - c * C < C ? n - c * C : C;
     __syncthreads();                            // the chunk before is done with LDS
     if (threadIdx.x == 0) bad = 0;
@@ -312,168 +385,198 @@ __global__ __launch_bounds__(NT, 2) void linattn_kernel(Lin a) {
     rv.store(vt);
     if (held != len) {
       held = len;
+      gone = power(l2, len);
       for (int x = threadIdx.x; x < C; x += NT) wt[x] = x < len ? R.update * power(l2, len - 1 - x + R.shift) : 0.0f;
     }
     const bool odd = OUT && rv.lost();
     __syncthreads();
     if (odd) bad = 1;
     if (c + 1 < live) load(c + 1);
+    // Operands are read from LDS a batch ahead of the products that take them: read and waited for one by one, they
+    // made the waits half as long again.
+    f32x4 acc[CT];
+    Frag<T> vf[C / KS];
+    float since[CT];
     if constexpr (OUT) {
-      // pt[t][s] = intra lambda^(t - s) q_t k_s for s <= t; tiles dealt to the waves
-      for (int tile = w; tile < CT * CT; tile += 4) {
-        const int ti = CT == 4 ? w : tile / CT, si = CT == 4 ? tile / 4 : tile % CT;
-        if (si > ti) continue;
-        f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+      // pt[t][s] = intra lambda^(t - s) q_t k_s for s <= t
+      if (w < TILES) {
+        const int ti = w < 1 ? 0 : 1, si = w < 2 ? 0 : 1, t = ti * 16 + i;
+        constexpr int B = KD / KS < 4 ? KD / KS : 4;
+        f32x4 p = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int kk = 0; kk < KD / KS; ++kk)
-          mma(row_frag(kt + (si * 16 + i) * LK + kk * KS + g * VE), row_frag(qt + (ti * 16 + i) * LK + kk * KS + g * VE),
-              acc);
-        const int t = ti * 16 + i;
+        for (int k0 = 0; k0 < KD / KS; k0 += B) {
+          if (k0 * KS >= R.inner) continue;
+          Frag<T> kf[B], qf[B];
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int apart = t - (si * 16 + 4 * g + r);
-          acc[r] = apart >= 0 ? acc[r] * (R.intra * power(l2, apart < 0 ? 0 : apart)) : 0.0f;
+          for (int kk = 0; kk < B; ++kk) {
+            kf[kk] = row_frag(kt + (si * 16 + i) * LK + (k0 + kk) * KS + g * VE);
+            qf[kk] = row_frag(qt + t * LQ + (k0 + kk) * KS + g * VE);
+          }
+          phase_end();
+#pragma unroll
+          for (int kk = 0; kk < B; ++kk) mma(kf[kk], qf[kk], p);
         }
-        put4(pt + t * LP + si * 16 + 4 * g, acc);
+        const int apart = t - si * 16 - 4 * g;  // of the first of the lane's four
+        if (ti == si) {
+#pragma unroll
+          for (int r = 0; r < 4; ++r) p[r] = apart >= r ? p[r] * near[C - 1 - (apart >= r ? apart - r : 0)] : 0.0f;
+        } else {
+#pragma unroll
+          for (int r = 0; r < 4; ++r) p[r] *= near[C - 1 - apart + r];
+        }
+        put4(pt + t * LP + si * 16 + 4 * g, p);
       }
-      __syncthreads();
     }
-    const bool some = OUT && bad != 0;
-    Frag<T> vf[C / KS][ET];
+    if (mine) {
+      if constexpr (OUT) {
+        // from the state before the chunk
 #pragma unroll
-    for (int kb = 0; kb < C / KS; ++kb)
+        for (int ti = 0; ti < CT; ++ti) acc[ti] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        Frag<T> qf[2][CT];
+        auto queries = [&](int kk) {
 #pragma unroll
-      for (int et = 0; et < ET; ++et)
-        column_frag(vf[kb][et], vt + kb * KS * LV + w * 16 * ET + 4 * et, LV, i, g, 4 * ET);
-    if constexpr (OUT) {
-      Frag<T> sf[KD / KS][ET];
-#pragma unroll
-      for (int kk = 0; kk < KD / KS; ++kk)
-#pragma unroll
-        for (int et = 0; et < ET; ++et) state_frag(sf[kk][et], S, kk, et);
-#pragma unroll
-      for (int ti = 0; ti < CT; ++ti) {
-        const int t = ti * 16 + i;
-        f32x4 acc[ET];
-#pragma unroll
-        for (int et = 0; et < ET; ++et) acc[et] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+          for (int ti = 0; ti < CT; ++ti) qf[kk & 1][ti] = row_frag(qt + (ti * 16 + i) * LQ + kk * KS + g * VE);
+        };
+        queries(0);
 #pragma unroll
         for (int kk = 0; kk < KD / KS; ++kk) {
-          Frag<T> qf;
-          query_frag(qf, qt + t * LK, kk, g);
+          if (kk * KS >= R.inner) continue;
+          if (kk + 1 < KD / KS) queries(kk + 1);
+          Frag<T> sf;
+          state_frag(sf, S, kk);
+          phase_end();
 #pragma unroll
-          for (int et = 0; et < ET; ++et) mma(sf[kk][et], qf, acc[et]);
+          for (int ti = 0; ti < CT; ++ti) mma(sf, qf[kk & 1][ti], acc[ti]);
+          phase_end();
         }
-        const float from = R.inter * power(l2, t + 1 - R.shift);
 #pragma unroll
-        for (int et = 0; et < ET; ++et) acc[et] *= from;
+        for (int ti = 0; ti < CT; ++ti) since[ti] = from[ti * 16 + i];
+      }
 #pragma unroll
-        for (int kb = 0; kb < C / KS; ++kb) {
-          if (kb * KS >= 16 * (ti + 1)) continue;
-          const Frag<T> pf = row_frag(pt + t * LP + kb * KS + g * VE);
+      for (int kb = 0; kb < C / KS; ++kb) column_frag(vf[kb], vt + kb * KS * LV + w * 16, LV, i, g, 4);
+    }
+    if (OUT) __syncthreads();                   // pt is complete
+    if (!mine) continue;
+    if constexpr (OUT) {
+      if (bad == 0) {
+        Frag<T> pf[CT][C / KS];
 #pragma unroll
-          for (int et = 0; et < ET; ++et) {
-            Frag<T> vv = vf[kb][et];
-            if (some) finite_only(vv);
-            mma(vv, pf, acc[et]);
+        for (int ti = 0; ti < CT; ++ti)
+#pragma unroll
+          for (int kb = 0; kb < C / KS; ++kb)
+            if (kb * KS < 16 * (ti + 1)) pf[ti][kb] = row_frag(pt + (ti * 16 + i) * LP + kb * KS + g * VE);
+#pragma unroll
+        for (int ti = 0; ti < CT; ++ti)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) acc[ti][r] *= since[ti];
+        phase_end();
+#pragma unroll
+        for (int kb = 0; kb < C / KS; ++kb)
+#pragma unroll
+          for (int ti = 0; ti < CT; ++ti)
+            if (kb * KS < 16 * (ti + 1)) mma(vf[kb], pf[ti][kb], acc[ti]);
+      } else {
+        // an infinite or NaN value reaches the steps from its own on, which a product with the zeros above the
+        // diagonal does not keep to: step by step
+#pragma unroll
+        for (int ti = 0; ti < CT; ++ti) {
+#pragma unroll
+          for (int x = 0; x < 4; ++x) acc[ti][x] *= since[ti];
+          for (int s = 0; s <= ti * 16 + i; ++s) {
+            const float p = St<T>::ld(pt, (ti * 16 + i) * LP + s);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) acc[ti][x] = fmaf(p, St<T>::ld(vt, s * LV + w * 16 + 4 * g + x), acc[ti][x]);
           }
         }
-        if (some) {
-          // an infinite or NaN value reaches the steps from its own on, which a product with the zeros above the
-          // diagonal does not keep to: such values one by one
-          for (int s = 0; s <= t; ++s) {
-            const float p = St<T>::ld(pt, t * LP + s);
+      }
+      phase_end();
+    }
+    // the state after the chunk: batches of four of its tiles and one summation step
+    constexpr int B = 4, PB = KT / B, BATCHES = C / KS * PB;
+    Frag<T> kf[2][B];
+    auto keys = [&](int u) {
 #pragma unroll
-            for (int x = 0; x < 4 * ET; ++x) {
-              const float val = St<T>::ld(vt, s * LV + w * 16 * ET + 4 * ET * g + x);
-              if (lost(val)) acc[x / 4][x % 4] += p * val;
+      for (int x = 0; x < B; ++x) key_frag(kf[u & 1][x], kt + u / PB * KS * LK, LK, u % PB * B + x, i, g);
+    };
+    keys(0);
+    if constexpr (OUT) {
+#pragma unroll
+      for (int ti = 0; ti < CT; ++ti)
+        if (ti * 16 + i < len) put(orow + (int64_t)(c * C + ti * 16) * ostep, acc[ti]);
+    }
+#pragma unroll
+    for (int dt = 0; dt < KT; ++dt) S[dt] *= gone;
+    Frag<T> part[2];
+#pragma unroll
+    for (int u = 0; u < BATCHES; ++u) {
+      const int kb = u / PB, dt = u % PB * B;
+      if (dt == 0) {
+        float ws[VE];
+#pragma unroll
+        for (int x = 0; x < VE; x += 4) *(f32x4*)(ws + x) = *(const f32x4*)&wt[kb * KS + g * VE + x];
+        if constexpr (sizeof(T) == 2) {
+          float rest[VE];
+          split(vf[kb], ws, part, rest);
+          if (exact) {
+            Frag<T> last;
+#pragma unroll
+            for (int x = 0; x < VE; ++x) last.v[x] = (__bf16)rest[x];
+#pragma unroll
+            for (int d = 0; d < KT; ++d) {
+              Frag<T> f;
+              key_frag(f, kt + kb * KS * LK, LK, d, i, g);
+              mma(f, last, S[d]);
             }
           }
-        }
-        put(c, t, acc);
-      }
-    }
-    // the state after the chunk
-    const float gone = power(l2, len);
+        } else {
 #pragma unroll
-    for (int dt = 0; dt < KT; ++dt)
-#pragma unroll
-      for (int et = 0; et < ET; ++et) S[dt][et] *= gone;
-#pragma unroll
-    for (int kb = 0; kb < C / KS; ++kb) {
-      if constexpr (sizeof(T) == 2) {
-        Frag<T> part[ET][3];
-        float ws[VE];
-        *(f32x4*)ws = *(const f32x4*)&wt[kb * KS + g * VE];
-        *(f32x4*)(ws + 4) = *(const f32x4*)&wt[kb * KS + g * VE + 4];
-#pragma unroll
-        for (int et = 0; et < ET; ++et) split(vf[kb][et], ws, part[et]);
-#pragma unroll
-        for (int dt = 0; dt < KT; ++dt) {
-          Frag<T> kf;
-          column_frag(kf, kt + kb * KS * LK + dt * 16, LK, i, g, 4);
-#pragma unroll
-          for (int et = 0; et < ET; ++et) {
-            if (exact) mma(kf, part[et][2], S[dt][et]);
-            mma(kf, part[et][1], S[dt][et]);
-            mma(kf, part[et][0], S[dt][et]);
-          }
-        }
-      } else {
-        const f32x4 ws = *(const f32x4*)&wt[kb * KS + g * VE];
-#pragma unroll
-        for (int et = 0; et < ET; ++et)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) vf[kb][et].v[e] *= ws[e];
-#pragma unroll
-        for (int dt = 0; dt < KT; ++dt) {
-          Frag<T> kf;
-          column_frag(kf, kt + kb * KS * LK + dt * 16, LK, i, g, 4);
-#pragma unroll
-          for (int et = 0; et < ET; ++et) mma(kf, vf[kb][et], S[dt][et]);
+          for (int x = 0; x < VE; ++x) part[0].v[x] = vf[kb].v[x] * ws[x];
         }
       }
+      if (u + 1 < BATCHES) keys(u + 1);
+      phase_end();
+      if (dt * 16 < R.inner) {
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+          for (int x = 0; x < B; ++x) mma(kf[u & 1][x], part[1], S[dt + x]);
+        }
+#pragma unroll
+        for (int x = 0; x < B; ++x) mma(kf[u & 1][x], part[0], S[dt + x]);
+      }
+      phase_end();
     }
   }
   if constexpr (OUT) {
-    for (int c = c0 < live ? live : c0; c < c1; ++c) {              // chunks behind the sequence's end
-      for (int t = i; t < C; t += 16) {
-        f32x4 none[ET] = {};
-        put(c, t, none);
-      }
-    }
+    const int64_t last = (int64_t)c1 * C < a.length ? (int64_t)c1 * C : a.length;
+    for (int64_t t = (n > c0 * C ? n : c0 * C) + (lane & 15); t < last; t += 16)        // steps behind the sequence's end
+      put(start + t * R.os.step, f32x4{0.0f, 0.0f, 0.0f, 0.0f});
     if (R.sT != nullptr && seg == a.nseg - 1) {
 #pragma unroll
       for (int dt = 0; dt < KT; ++dt)
 #pragma unroll
-        for (int et = 0; et < ET; ++et)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int d = 16 * dt + 4 * g + r, e = se + 4 * et;
-            if (d < R.inner && e < R.value) R.sT[state + d * R.s_inner + e * R.s_value] = S[dt][et][r];
-          }
+        for (int r = 0; r < 4; ++r) {
+          const int d = state_row<T>(dt, lane >> 4) + r, x = e0 + (lane & 15);
+          if (d < R.inner && x < R.value) R.sT[state + d * R.s_inner + x * R.s_value] = S[dt][r];
+        }
     }
   } else {
 #pragma unroll
-    for (int dt = 0; dt < KT; ++dt)
-#pragma unroll
-      for (int et = 0; et < ET; ++et) *(f32x4*)(segment + (dt * ET + et) * 256) = S[dt][et];
+    for (int dt = 0; dt < KT; ++dt) *(f32x4*)(segment + dt * 256) = S[dt];
   }
 }
 
 // The segments' states from zero become their first states: a thread takes one piece of four through the segments.
-template <int KD, int ET, int C>
+template <typename T, int KD, int NW>
 __global__ __launch_bounds__(NT) void linattn_chain_kernel(Lin a) {
   constexpr int KT = KD / 16;
   const Role& R = a.role[blockIdx.y];
-  const int64_t pieces = (int64_t)R.blocks * 4 * KT * ET * 64;
-  const int per = (int)(pieces / NT);                         // workgroups of a head
+  const int per = R.blocks * NW * KT * 64 / NT;               // workgroups of a head
+  const int64_t pieces = (int64_t)per * NT;
   const int bh = blockIdx.x / per;
   if (bh >= a.batch * a.heads) return;                        // a role with fewer blocks
-  const int x = (blockIdx.x % per) * NT + threadIdx.x;
-  const int lane = x % 64, et = x / 64 % ET, dt = x / 64 / ET % KT, wave = x / 64 / ET / KT;   // wave of all blocks
-  const int i = lane & 15, g = lane >> 4;
-  const int d = 16 * dt + 4 * g, e = wave * 16 * ET + 4 * ET * (i >> 2) + 4 * et + (i & 3);
+  const int x = blockIdx.x % per * NT + threadIdx.x;
+  const int lane = x % 64, dt = x / 64 % KT, wave = x / 64 / KT;         // wave of all blocks
+  const int d = state_row<T>(dt, lane >> 4), e = wave * 16 + (lane & 15);
   f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
   if (R.s0 != nullptr) {
 #pragma unroll
@@ -484,14 +587,13 @@ __global__ __launch_bounds__(NT) void linattn_chain_kernel(Lin a) {
   const int b = bh / a.heads, n = steps_of(a.lengths, b, a.length);
   const float l2 = log2_decay(a.decay, bh % a.heads);
   f32x4* p = (f32x4*)R.seg + (int64_t)bh * a.nseg * pieces + x;
+  f32x4 u = p[0];
   for (int j = 0; j < a.nseg; ++j) {
-    f32x4 u = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (j + 1 < a.nseg) u = p[j * pieces];
+    const f32x4 next = j + 2 < a.nseg ? p[(j + 1) * pieces] : u;
     p[j * pieces] = s;
-    const int64_t from = (int64_t)j * a.seg_chunks * C, steps = n - from;
-    const int64_t most = (int64_t)a.seg_chunks * C;
-    const int len = steps < 0 ? 0 : steps < most ? (int)steps : (int)most;
-    s = s * power(l2, len) + u;
+    const int64_t most = (int64_t)a.seg_chunks * C, steps = n - j * most;
+    s = s * power(l2, steps < 0 ? 0 : steps < most ? (int)steps : (int)most) + u;
+    u = next;
   }
 }
 
@@ -559,51 +661,64 @@ __global__ __launch_bounds__(NT) void linattn_step_kernel(Lin a, int lanes) {
     St<T>::st(R.o, b * R.os.batch + h * R.os.head + e + x, live ? o[x] * R.inter : 0.0f);
 }
 
-// gradients of keys and values that heads share: out = the heads' sum, in their order
+// Gradients of keys and values that heads share: the heads' sum, in their order, four values a thread.
 template <typename T>
-__global__ __launch_bounds__(NT) void linattn_heads_kernel(const float* part, void* out, pnn_head_stride st, int64_t rows,
-                                                           int length, int kv, int group, int width) {
-  const int64_t x = (int64_t)blockIdx.x * NT + threadIdx.x;
-  const int e = (int)(x % width);
-  const int64_t r = x / width;                            // (batch, step, shared head)
+__global__ __launch_bounds__(NT) void linattn_heads_kernel(const float* part_k, const float* part_v, void* dk, void* dv,
+                                                           pnn_head_stride ks, pnn_head_stride vs, int64_t rows,
+                                                           int length, int kv, int group, int key_width,
+                                                           int value_width) {
+  const bool keys = blockIdx.y == 0;
+  const int width = keys ? key_width : value_width, pieces = (width + 3) / 4;
+  const int64_t x = (int64_t)blockIdx.x * NT + threadIdx.x, r = x / pieces;       // (batch, step, shared head)
+  const int e = (int)(x % pieces) * 4;
   if (r >= rows) return;
-  float s = 0.0f;
-  for (int j = 0; j < group; ++j) s += part[(r * group + j) * width + e];
-  const int64_t bt = r / kv;
-  St<T>::st(out, bt / length * st.batch + bt % length * st.step + r % kv * st.head + e, s);
+  const float* p = (keys ? part_k : part_v) + r * group * width + e;
+  const pnn_head_stride& st = keys ? ks : vs;
+  const int64_t bt = r / kv, o = bt / length * st.batch + bt % length * st.step + r % kv * st.head + e;
+  void* const out = keys ? dk : dv;
+  typedef f32x4 VM __attribute__((aligned(4)));
+  if (e + 4 <= width) {
+    f32x4 s = *(const VM*)p;
+    for (int j = 1; j < group; ++j) s += *(const VM*)(p + (int64_t)j * width);
+    put_any((T*)out + o, s);
+  } else {
+    for (int c = 0; e + c < width; ++c) {
+      float s = p[c];
+      for (int j = 1; j < group; ++j) s += p[(int64_t)j * width + c];
+      St<T>::st(out, o + c, s);
+    }
+  }
 }
 
-template <typename T, int KD, int ET>
+template <typename T, int KD, int NW>
 int launch_roles(Lin& a, hipStream_t s) {
-  constexpr int C = lin_chunk(sizeof(T), KD);
-  int64_t grid = 0;
-  int most = 0;
-  for (int z = 0; z < a.roles; ++z) {
-    Role& R = a.role[z];
-    R.first = (int)grid;
-    grid += (int64_t)a.batch * a.heads * a.nseg * R.blocks;
-    if (R.blocks > most) most = R.blocks;
-  }
+  const dim3 grid((unsigned)(cdiv64(a.items, 8) * 8 * a.roles * a.most)), threads(64 * NW);
   if (a.nseg > 1) {
-    hipLaunchKernelGGL((linattn_kernel<T, KD, ET, C, false>), dim3((unsigned)grid), dim3(NT), 0, s, a);
-    const unsigned per = (unsigned)(most * KD / 16 * ET);     // 4 KT ET 64 / NT a block
-    hipLaunchKernelGGL((linattn_chain_kernel<KD, ET, C>), dim3(per * a.batch * a.heads, a.roles), dim3(NT), 0, s, a);
+    hipLaunchKernelGGL((linattn_kernel<T, KD, NW, false>), grid, threads, 0, s, a);
+    const unsigned per = (unsigned)(a.most * (NW * (KD / 16) * 64 / NT));
+    hipLaunchKernelGGL((linattn_chain_kernel<T, KD, NW>), dim3(per * a.batch * a.heads, a.roles), dim3(NT), 0, s, a);
   }
-  hipLaunchKernelGGL((linattn_kernel<T, KD, ET, C, true>), dim3((unsigned)grid), dim3(NT), 0, s, a);
+  hipLaunchKernelGGL((linattn_kernel<T, KD, NW, true>), grid, threads, 0, s, a);
   return (int)hipGetLastError();
 }
 
 template <typename T>
-int launch_shape(Lin& a, const LinShape& p, hipStream_t s) {
-  if (p.pad == 64) return p.tiles == 1 ? launch_roles<T, 64, 1>(a, s) : launch_roles<T, 64, 2>(a, s);
-  if (p.pad == 128) return p.tiles == 1 ? launch_roles<T, 128, 1>(a, s) : launch_roles<T, 128, 2>(a, s);
-  return launch_roles<T, 256, 1>(a, s);
+int launch_type(Lin& a, const LinShape& p, hipStream_t s) {
+  if (p.pad == 64) return p.waves == 4 ? launch_roles<T, 64, 4>(a, s) : launch_roles<T, 64, 8>(a, s);
+  if (p.pad == 128) return p.waves == 4 ? launch_roles<T, 128, 4>(a, s) : launch_roles<T, 128, 8>(a, s);
+  return p.waves == 4 ? launch_roles<T, 256, 4>(a, s) : launch_roles<T, 256, 8>(a, s);
 }
 
-int launch_any(int dtype, Lin& a, const LinShape& p, hipStream_t s) {
+int launch_shape(int dtype, Lin& a, const LinShape& p, hipStream_t s) {
   a.nseg = p.segments;
   a.seg_chunks = p.seg_chunks;
-  return dtype == PNN_F32 ? launch_shape<float>(a, p, s) : launch_shape<uint16_t>(a, p, s);
+  a.most = 0;
+  for (int z = 0; z < a.roles; ++z) {
+    a.role[z].blocks = lin_blocks(p, a.role[z].value);
+    if (a.role[z].blocks > a.most) a.most = a.role[z].blocks;
+  }
+  a.items = a.batch * a.heads * a.nseg;
+  return dtype == PNN_F32 ? launch_type<float>(a, p, s) : launch_type<uint16_t>(a, p, s);
 }
 
 Lin common(const pnn_linattn_desc& d, const float* decay, const int32_t* lengths) {
@@ -644,10 +759,9 @@ int launch_linattn_fwd(const pnn_linattn_desc& d, const void* q, const void* k, 
 #undef STEP
     return (int)hipGetLastError();
   }
-  const LinShape p = lin_shape(d, d.key_width, d.value_width, 1);
-  R.blocks = p.blocks;
+  const LinShape p = lin_shape(d, false);
   R.seg = p.segments > 1 ? (float*)ws : nullptr;
-  return launch_any(d.dtype, a, p, s);
+  return launch_shape(d.dtype, a, p, s);
 }
 
 int launch_linattn_bwd(const pnn_linattn_desc& d, const void* q, const void* k, const void* v, const float* decay,
@@ -657,9 +771,34 @@ int launch_linattn_bwd(const pnn_linattn_desc& d, const void* q, const void* k, 
   const LinBwd w = lin_bwd(d);
   char* const base = (char*)ws;
   Lin a = common(d, decay, lengths);
-  Role &Q = a.role[0], &K = a.role[1];
-  a.roles = 2;
-  // dq_t = scale sum_{s <= t} lambda^(t - s) (do_t v_s) k_s + ..: inner width that of the values
+  a.roles = 3;
+  const bool cut = w.shape.segments > 1, shared = group > 1;
+  // dk_s = sum_{t >= s} lambda^(t - s) (v_s do_t) scale q_t + lambda^(n - 1 - s) v_s dS_T
+  Role& K = a.role[0];
+  K.q = v, K.k = dout, K.v = q, K.o = shared ? (void*)(base + w.part_k) : dk;
+  K.qs = d.v, K.ks = d.dout, K.vs = d.q, K.os = shared ? lin_dense(d, d.key_width) : d.dk;
+  K.q_group = group, K.k_group = K.v_group = 1;
+  K.s0 = dsT;
+  K.s_inner = 1, K.s_value = d.value_width;
+  K.inner = (int)d.value_width, K.value = (int)d.key_width;
+  K.intra = K.update = d.scale, K.inter = 1.0f;
+  K.shift = 1;
+  K.o_float = shared;
+  K.seg = cut ? (float*)(base + w.seg_k) : nullptr;
+  // dv_s = sum_{t >= s} lambda^(t - s) (k_s q_t) scale do_t + lambda^(n - 1 - s) k_s dS_T; dS_0
+  Role& V = a.role[1];
+  V.q = k, V.k = q, V.v = dout, V.o = shared ? (void*)(base + w.part_v) : dv;
+  V.qs = d.k, V.ks = d.q, V.vs = d.dout, V.os = shared ? lin_dense(d, d.value_width) : d.dv;
+  V.q_group = group, V.k_group = V.v_group = 1;
+  V.s0 = dsT, V.sT = ds0;
+  V.s_inner = d.value_width, V.s_value = 1;
+  V.inner = (int)d.key_width, V.value = (int)d.value_width;
+  V.intra = V.update = d.scale, V.inter = 1.0f;
+  V.shift = 1;
+  V.o_float = shared;
+  V.seg = cut ? (float*)(base + w.seg_v) : nullptr;
+  // dq_t = scale sum_{s <= t} lambda^(t - s) (do_t v_s) k_s + scale lambda^(t + 1) S_0 do_t
+  Role& Q = a.role[2];
   Q.q = dout, Q.k = v, Q.v = k, Q.o = dq;
   Q.qs = d.dout, Q.ks = d.v, Q.vs = d.k, Q.os = d.dq;
   Q.q_group = 1, Q.k_group = Q.v_group = group;
@@ -667,50 +806,18 @@ int launch_linattn_bwd(const pnn_linattn_desc& d, const void* q, const void* k, 
   Q.s_inner = 1, Q.s_value = d.value_width;
   Q.inner = (int)d.value_width, Q.value = (int)d.key_width;
   Q.intra = Q.inter = d.scale, Q.update = 1.0f;
-  Q.blocks = w.wide.blocks;
-  Q.seg = w.wide.segments > 1 ? (float*)(base + w.seg_q) : nullptr;
-  // dk_s = sum_{t >= s} lambda^(t - s) (v_s do_t) scale q_t + lambda^(n - 1 - s) v_s dS_T
-  K.q = v, K.k = dout, K.v = q, K.o = group > 1 ? (void*)(base + w.part_k) : dk;
-  K.qs = d.v, K.ks = d.dout, K.vs = d.q, K.os = group > 1 ? lin_dense(d, d.key_width) : d.dk;
-  K.q_group = group, K.k_group = K.v_group = 1;
-  K.s0 = dsT;
-  K.s_inner = 1, K.s_value = d.value_width;
-  K.inner = (int)d.value_width, K.value = (int)d.key_width;
-  K.intra = K.update = d.scale, K.inter = 1.0f;
-  K.shift = 1;
-  K.o_float = group > 1;
-  K.blocks = w.wide.blocks;
-  K.seg = w.wide.segments > 1 ? (float*)(base + w.seg_k) : nullptr;
-  if (const int e = launch_any(d.dtype, a, w.wide, s)) return e;
-  // dv_s = sum_{t >= s} lambda^(t - s) (k_s q_t) scale do_t + lambda^(n - 1 - s) k_s dS_T; dS_0
-  Lin c = common(d, decay, lengths);
-  Role& V = c.role[0];
-  c.roles = 1;
-  V.q = k, V.k = q, V.v = dout, V.o = group > 1 ? (void*)(base + w.part_v) : dv;
-  V.qs = d.k, V.ks = d.q, V.vs = d.dout, V.os = group > 1 ? lin_dense(d, d.value_width) : d.dv;
-  V.q_group = group, V.k_group = V.v_group = 1;
-  V.s0 = dsT, V.sT = ds0;
-  V.s_inner = d.value_width, V.s_value = 1;
-  V.inner = (int)d.key_width, V.value = (int)d.value_width;
-  V.intra = V.update = d.scale, V.inter = 1.0f;
-  V.shift = 1;
-  V.o_float = group > 1;
-  V.blocks = w.deep.blocks;
-  V.seg = w.deep.segments > 1 ? (float*)(base + w.seg_v) : nullptr;
-  if (const int e = launch_any(d.dtype, c, w.deep, s)) return e;
-  if (group > 1) {
+  Q.seg = cut ? (float*)(base + w.seg_q) : nullptr;
+  if (const int e = launch_shape(d.dtype, a, w.shape, s)) return e;
+  if (shared && d.length > 0) {
     const int64_t rows = d.batch * d.length * d.kv_heads;
-    auto sum = [&](const float* part, void* out, const pnn_head_stride& st, int64_t width) {
-      const dim3 grid((unsigned)cdiv64(rows * width, NT));
-      if (d.dtype == PNN_F32)
-        hipLaunchKernelGGL((linattn_heads_kernel<float>), grid, dim3(NT), 0, s, part, out, st, rows, (int)d.length,
-                           (int)d.kv_heads, group, (int)width);
-      else
-        hipLaunchKernelGGL((linattn_heads_kernel<uint16_t>), grid, dim3(NT), 0, s, part, out, st, rows, (int)d.length,
-                           (int)d.kv_heads, group, (int)width);
-    };
-    sum((const float*)(base + w.part_k), dk, d.dk, d.key_width);
-    sum((const float*)(base + w.part_v), dv, d.dv, d.value_width);
+    const int64_t wide = d.key_width > d.value_width ? d.key_width : d.value_width;
+    const dim3 grid((unsigned)cdiv64(rows * cdiv64(wide, 4), NT), 2);
+#define HEADS(T) hipLaunchKernelGGL((linattn_heads_kernel<T>), grid, dim3(NT), 0, s, (const float*)(base + w.part_k), \
+    (const float*)(base + w.part_v), dk, dv, d.dk, d.dv, rows, (int)d.length, (int)d.kv_heads, group, \
+    (int)d.key_width, (int)d.value_width)
+    if (d.dtype == PNN_F32) HEADS(float);
+    else HEADS(uint16_t);
+#undef HEADS
   }
   return (int)hipGetLastError();
 }

@@ -156,56 +156,59 @@ int launch_distill(const pnn_distill_desc& d, const void* logits, const int32_t*
 
 // ---- linear attention ----
 constexpr int LIN_MAX_WIDTH = PNN_LINATTN_MAX_WIDTH;
-constexpr int64_t LIN_WGS = 256;           // workgroups below which sequences are cut into segments
-// steps of a chunk, by the bytes of an element and the padded inner width: what fits two workgroups into a CU's LDS
-constexpr int lin_chunk(int size, int pad) { return size == 2 && pad <= 128 ? 64 : 32; }
-// How one of the sums runs: inner width padded to `pad`, 64 x tiles value columns to a workgroup, segments of a sequence
+constexpr int LIN_CHUNK = 32;              // steps of a chunk
+constexpr int64_t LIN_FEW = 256, LIN_MANY = 512;  // workgroups below which sequences are cut, and to how many
+// How the sums of a direction run: widths summed over padded to `pad`, workgroups of as many waves with 16 value columns
+// each, segments of a sequence.  One shape for all three sums of the backward, which run side by side in a launch.
 struct LinShape {
-  int pad, tiles, blocks, segments, seg_chunks;
-  int64_t bytes;                           // of the segments' states
+  int pad, waves, segments, seg_chunks;
 };
-inline LinShape lin_shape(const pnn_linattn_desc& d, int64_t inner, int64_t value, int roles) {
+inline int lin_blocks(const LinShape& p, int64_t value) { return (int)cdiv64(value, 16 * p.waves); }
+inline LinShape lin_shape(const pnn_linattn_desc& d, bool backward) {
   LinShape p;
+  const int64_t K = d.key_width, V = d.value_width, most = K > V ? K : V;
+  const int64_t inner = backward ? most : K, value = backward ? most : V;
   p.pad = inner <= 64 ? 64 : inner <= 128 ? 128 : 256;
-  p.tiles = value <= 64 || p.pad == 256 ? 1 : 2;
-  p.blocks = (int)cdiv64(value, 64 * p.tiles);
-  const int64_t chunks = cdiv64(d.length, lin_chunk(d.dtype == PNN_F32 ? 4 : 2, p.pad));
-  const int64_t wgs = d.batch * d.heads * p.blocks * roles;
+  p.waves = value <= 64 ? 4 : 8;
+  const int64_t chunks = cdiv64(d.length, LIN_CHUNK);
+  const int64_t wgs = d.batch * d.heads * (lin_blocks(p, V) + (backward ? 2 * lin_blocks(p, K) : 0));
   int64_t seg = 1;
-  if (wgs > 0 && wgs < LIN_WGS) {
-    seg = cdiv64(2 * LIN_WGS, wgs);
-    if (seg > chunks / 4) seg = chunks / 4;
+  if (wgs > 0 && wgs < LIN_FEW) {
+    seg = cdiv64(LIN_MANY, wgs);
+    if (seg > chunks / 8) seg = chunks / 8;
     if (seg < 1) seg = 1;
   }
   p.seg_chunks = (int)(chunks > 0 ? cdiv64(chunks, seg) : 1);
   p.segments = (int)(chunks > 0 ? cdiv64(chunks, p.seg_chunks) : 1);
-  p.bytes = p.segments > 1 ? d.batch * d.heads * p.segments * p.blocks * p.pad * 64 * p.tiles * 4 : 0;
   return p;
 }
+// bytes of the segments' states of a sum over values of `value` columns
+inline int64_t lin_seg_bytes(const pnn_linattn_desc& d, const LinShape& p, int64_t value) {
+  return p.segments > 1 ? d.batch * d.heads * p.segments * lin_blocks(p, value) * p.pad * 16 * p.waves * 4 : 0;
+}
 inline int64_t lin_fwd_bytes(const pnn_linattn_desc& d) {
-  return d.length == 1 ? 0 : lin_shape(d, d.key_width, d.value_width, 1).bytes;
+  return d.length == 1 ? 0 : lin_seg_bytes(d, lin_shape(d, false), d.value_width);
 }
 inline pnn_head_stride lin_dense(const pnn_linattn_desc& d, int64_t width) {
   return pnn_head_stride{d.length * d.heads * width, d.heads * width, width};
 }
 // Workspace of the backward: the three sums' segments; gradients of single heads where keys and values are shared
 struct LinBwd {
-  LinShape wide, deep;                     // dq and dk; dv
+  LinShape shape;
   int64_t seg_q, seg_k, seg_v, part_k, part_v, bytes;
 };
 inline LinBwd lin_bwd(const pnn_linattn_desc& d) {
   LinBwd w;
-  w.wide = lin_shape(d, d.value_width, d.key_width, 2);
-  w.deep = lin_shape(d, d.key_width, d.value_width, 1);
+  w.shape = lin_shape(d, true);
   int64_t o = 0;
   auto take = [&](int64_t bytes) {
     const int64_t at = o;
     o += round256(bytes);
     return at;
   };
-  w.seg_q = take(w.wide.bytes);
-  w.seg_k = take(w.wide.bytes);
-  w.seg_v = take(w.deep.bytes);
+  w.seg_q = take(lin_seg_bytes(d, w.shape, d.key_width));
+  w.seg_k = take(lin_seg_bytes(d, w.shape, d.key_width));
+  w.seg_v = take(lin_seg_bytes(d, w.shape, d.value_width));
   const int64_t steps = d.heads > d.kv_heads ? d.batch * d.length * d.heads * 4 : 0;
   w.part_k = take(steps * d.key_width);
   w.part_v = take(steps * d.value_width);
