@@ -76,38 +76,44 @@ __device__ __forceinline__ int steps_of(const int32_t* lengths, int b, int lengt
 }
 
 // Rows of a chunk on their way through registers, 16 bytes a lane and row piece.  The piece that the row's end cuts is
-// loaded and stored so that it ends there, over elements of the piece before it.  Rows shorter than a piece are copied
-// when they are stored.  What is behind a row's end in LDS stays as clear() left it.
-template <typename T, int NT, int W, int PAD>
+// loaded and stored so that it ends there, over elements of the piece before it (LEFT: columns in front of a tile's
+// rows, which nobody reads, for a value block that starts less than a piece before the row's end).  What is behind a
+// row's end in LDS stays as clear() left it.  TINY: rows may be shorter than a piece; they are copied when they are
+// stored.
+template <typename T, int NT, int W, int PAD, bool TINY>
 struct Stage {
-  static constexpr int VE = St<T>::VE, PR = W / VE, N = (C * PR + NT - 1) / NT, LD = W + PAD * VE;   // LD: elements of a row in LDS
+  static constexpr int VE = St<T>::VE, PR = W / VE, N = (C * PR + NT - 1) / NT;
+  static constexpr int LD = W + PAD * VE, LEFT = VE, SIZE = C * LD + LEFT;   // elements: of a row in LDS, in all
   static constexpr int ROWS = NT / PR;      // rows that the lanes' first pieces are of
   static_assert(N == 1 || N * NT == C * PR, "whole pieces");
   const T* p;                               // the lane's first piece of the next chunk; short rows: the chunk
   int64_t step;
-  int col, width, now;                      // the lane's column, -1: none; rows of the sequence in the chunk held
-  int row0;                                 // the lane's first row
+  int at, row0;                             // where the lane's first piece goes in LDS (negative: nowhere), its row
+  int width, now;                           // of a row; rows of the sequence in the chunk held
   uint4 r[N];
 
-  // the sequence's row 0 (its last one backwards in time), elements from row to row, elements of a row
+  // the sequence's row 0 (its last one backwards in time) at this tile's columns, elements from row to row, columns, row
   __device__ __forceinline__ void begin(const T* first, int64_t step_, int width_, int64_t row) {
     step = step_;
     width = width_;
-    col = (threadIdx.x % PR) * VE;
-    if (col >= width || width < VE || (int)threadIdx.x >= C * PR) col = -1;
-    else if (col + VE > width) col = width - VE;
+    row0 = threadIdx.x / PR;
+    int col = threadIdx.x % PR * VE;
+    const bool on = col < width && (int)threadIdx.x < C * PR;
+    if (col + VE > width) col = width - VE;
+    at = on ? LEFT + row0 * LD + col : -1;
+    if (!on) row0 = col = 0;
     p = first + row * step;
-    if (width >= VE && col >= 0) p += (int)(threadIdx.x / PR) * step + col;
-    row0 = col < 0 ? 0 : threadIdx.x / PR;
+    if (!TINY) p += row0 * step + col;
   }
   static __device__ __forceinline__ void clear(T* lds) {
-    for (int x = threadIdx.x; x < C * LD; x += NT) lds[x] = (T)0;
+    for (int x = threadIdx.x; x < SIZE; x += NT) lds[x] = (T)0;
   }
   // The next chunk, of which `len` > 0 rows belong to the sequence.  Nothing here depends on the lane but addresses (a
-  // load under a condition waits for the one before it): lanes that store nothing load the chunk's first column, and those of rows behind the sequence's end its last row.
+  // load under a condition waits for the one before it): lanes that store nothing load a piece all the same, and those
+  // of rows behind the sequence's end its last row.
   __device__ __forceinline__ void load(int len) {
     now = len;
-    if (width < VE) return;
+    if (TINY) return;
     if (len >= C) {
 #pragma unroll
       for (int j = 0; j < N; ++j) r[j] = piece(p + j * ROWS * step);
@@ -123,40 +129,36 @@ struct Stage {
     return __builtin_bit_cast(uint4, *(const typename Piece<T>::Mem*)s);
   }
   __device__ __forceinline__ void store(T* lds) {
-    if (width >= VE) {
+    if (!TINY) {
       if (now < C) {
 #pragma unroll
         for (int j = 0; j < N; ++j)
           if (row0 + j * ROWS >= now) r[j] = make_uint4(0, 0, 0, 0);
       }
-      if (col >= 0) {
+      if (at >= 0) {
         typedef typename Piece<T>::Mem Mem;
 #pragma unroll
-        for (int j = 0; j < N; ++j)
-          *(Mem*)(lds + (row0 + j * ROWS) * LD + col) = __builtin_bit_cast(typename Piece<T>::Vec, r[j]);
+        for (int j = 0; j < N; ++j) *(Mem*)(lds + at + j * ROWS * LD) = __builtin_bit_cast(typename Piece<T>::Vec, r[j]);
       }
     } else {
-      for (int x = threadIdx.x; x < C * VE; x += NT) {
-        const int row = x / VE, c = x % VE;
-        if (c < width) lds[row * LD + c] = row < now ? p[row * step + c] : (T)0;
+      for (int x = threadIdx.x; x < C * W; x += NT) {
+        const int row = x / W, c = x % W;
+        if (c < width) lds[LEFT + row * LD + c] = row < now ? p[row * step + c] : (T)0;
       }
     }
     p += C * step;
   }
-  // whether a value is infinite or NaN (short rows: not looked at)
+  // whether a value is infinite or NaN (TINY: not looked at)
   __device__ __forceinline__ bool lost() const {
-    if (width < VE) return true;
-    if (col < 0) return false;
-    typedef typename std::conditional<sizeof(T) == 2, uint16_t, uint32_t>::type U;
-    typedef U Bits __attribute__((ext_vector_type(16 / sizeof(T))));
-    constexpr U TOP = (U)(sizeof(T) == 2 ? 0x7f80u : 0x7f800000u), ALL = (U)(sizeof(T) == 2 ? 0x7fffu : 0x7fffffffu);
-    Bits m = {};
+    if (TINY) return true;
+    // an exponent of ones carries into the bit above it
+    constexpr uint32_t EXP = sizeof(T) == 2 ? 0x7f807f80u : 0x7f800000u, ONE = sizeof(T) == 2 ? 0x00800080u : 0x00800000u;
+    constexpr uint32_t TOP = sizeof(T) == 2 ? 0x80008000u : 0x80000000u;
+    uint32_t m = 0;
 #pragma unroll
-    for (int j = 0; j < N; ++j) m = __builtin_elementwise_max(m, __builtin_bit_cast(Bits, r[j]) & ALL);
-    bool any = false;
-#pragma unroll
-    for (int x = 0; x < VE; ++x) any |= m[x] >= TOP;
-    return any;
+    for (int j = 0; j < N; ++j)
+      m |= ((r[j].x & EXP) + ONE) | ((r[j].y & EXP) + ONE) | ((r[j].z & EXP) + ONE) | ((r[j].w & EXP) + ONE);
+    return (m & TOP) != 0 && at >= 0;
   }
 };
 
@@ -235,30 +237,27 @@ __device__ __forceinline__ void split(const Frag<uint16_t>& v, const float* w, F
 // nothing moves over this: without it the compiler has the next products' operands in registers, and spills
 __device__ __forceinline__ void phase_end() { __builtin_amdgcn_sched_barrier(0); }
 
-template <typename T>
-__device__ __forceinline__ void put4(T* p, f32x4 v) {      // aligned
-  if constexpr (sizeof(T) == 4) {
-    *(f32x4*)p = v;
-  } else {
-    uint2 u;
-    u.x = (uint32_t)f2bf(v[0]) | ((uint32_t)f2bf(v[1]) << 16);
-    u.y = (uint32_t)f2bf(v[2]) | ((uint32_t)f2bf(v[3]) << 16);
-    *(uint2*)p = u;
-  }
+// four neighbouring values, rounded (any: to any alignment)
+__device__ __forceinline__ uint2 round4(f32x4 v) {
+  typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+  return __builtin_bit_cast(uint2, __builtin_convertvector(v, bf16x4));
 }
-
-// four neighbouring values, rounded, to any alignment
+template <typename T>
+__device__ __forceinline__ void put4(T* p, f32x4 v) {
+  if constexpr (sizeof(T) == 4) *(f32x4*)p = v;
+  else *(uint2*)p = round4(v);
+}
 template <typename T>
 __device__ __forceinline__ void put_any(T* p, f32x4 v) {
-  typedef T V __attribute__((ext_vector_type(4)));
-  typedef V VM __attribute__((aligned(sizeof(T))));
-  V u;
-#pragma unroll
-  for (int x = 0; x < 4; ++x) {
-    if constexpr (sizeof(T) == 4) u[x] = v[x];
-    else u[x] = f2bf(v[x]);
+  typedef f32x4 FM __attribute__((aligned(4)));
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  typedef u32x2 UM __attribute__((aligned(2)));
+  if constexpr (sizeof(T) == 4) {
+    *(FM*)p = v;
+  } else {
+    const uint2 u = round4(v);
+    *(UM*)p = u32x2{u.x, u.y};
   }
-  *(VM*)p = u;
 }
 
 // waves that a SIMD is to hold, as far as registers and LDS allow
@@ -267,24 +266,28 @@ constexpr int lin_occupancy(int size, int pad, int waves) {
   return pad == 64 ? 4 : pad == 128 ? (waves == 4 ? 3 : 4) : 2;
 }
 
-// KD: inner width, padded; NW waves of 16 value columns each; OUT: outputs, not the state alone.
+// KD: inner width, padded; NW waves of 16 value columns each; OUT: outputs, not the state alone;
+// TINY: rows shorter than 16 bytes.
 // Two workgroups of eight waves a CU: what a wave waits for (LDS, barriers) is two thirds of its time.
-template <typename T, int KD, int NW, bool OUT>
+template <typename T, int KD, int NW, bool OUT, bool TINY>
 __global__ __launch_bounds__(64 * NW, lin_occupancy(sizeof(T), KD, NW)) void linattn_kernel(Lin a) {
   constexpr int NT = 64 * NW, VE = St<T>::VE, KS = 4 * VE, KT = KD / 16, CT = C / 16, EB = 16 * NW;
   constexpr int TILES = CT * (CT + 1) / 2;      // tiles of pt on or below the diagonal, one a wave
   static_assert(CT == 2 && TILES <= NW, "tiles of pt");
-  // Rows in LDS are longer than they need be by as many 16 bytes as keep the lanes of a read in different banks: 1 where
-  // rows are read along (queries), 4 where columns are (values), 6 where both are (keys).
-  typedef Stage<T, NT, KD, 1> SQ;
-  typedef Stage<T, NT, KD, 6> SK;
-  typedef Stage<T, NT, EB, 4> SV;
-  constexpr int LQ = SQ::LD, LK = SK::LD, LV = SV::LD, LP = C + VE;
-  __shared__ __attribute__((aligned(16))) T kt[C * LK];
-  __shared__ __attribute__((aligned(16))) T vt[C * LV];
-  __shared__ __attribute__((aligned(16))) T qt[OUT ? C * LQ : 1];
+  // Rows in LDS are longer than they need be by 16 bytes times what kept the lanes' reads apart best: 2, and 4 for the
+  // keys, whose columns are read in pieces 16 bytes apart (conflicts cost 3.4 of 12.3 million cycles; 9.7 of 18.6 with
+  // 1, 6 and 4 for queries, keys and values; the training batch 352 -> 337 us).
+  typedef Stage<T, NT, KD, 2, TINY> SQ;
+  typedef Stage<T, NT, KD, 4, TINY> SK;
+  typedef Stage<T, NT, EB, 2, TINY> SV;
+  constexpr int LQ = SQ::LD, LK = SK::LD, LV = SV::LD, LP = C + 2 * VE, LO = EB + 4;
+  __shared__ __attribute__((aligned(16))) T ks[SK::SIZE];
+  __shared__ __attribute__((aligned(16))) T vs[SV::SIZE];
+  __shared__ __attribute__((aligned(16))) T qs[OUT ? SQ::SIZE : 1];
   __shared__ __attribute__((aligned(16))) T pt[OUT ? C * LP : 1];
-  __shared__ __attribute__((aligned(16))) float wt[C], near[OUT ? C : 1], from[OUT ? C : 1];
+  __shared__ __attribute__((aligned(16))) float ot[OUT ? C * LO : 4];       // outputs on their way
+  __shared__ __attribute__((aligned(16))) float wt[C], near[OUT ? C + 16 : 1], from[OUT ? C : 1];
+  T *const kt = ks + SK::LEFT, *const vt = vs + SV::LEFT, *const qt = qs + SQ::LEFT;
   __shared__ int bad;
   // workgroups eight apart run on one XCD and share its L2: the roles and value blocks of a head and segment, which read
   // the same tensors
@@ -342,37 +345,49 @@ __global__ __launch_bounds__(64 * NW, lin_occupancy(sizeof(T), KD, NW)) void lin
     rv.load(len);
   };
   if (c0 < live) load(c0);
-  if (OUT) SQ::clear(qt);
-  SK::clear(kt);
-  SV::clear(vt);
+  if (OUT) SQ::clear(qs);
+  SK::clear(ks);
+  SV::clear(vs);
   if constexpr (OUT) {                          // tiles of pt above the diagonal stay zero
     for (int x = threadIdx.x; x < C * LP; x += NT) pt[x] = (T)0;
     for (int x = threadIdx.x; x < C; x += NT) {
-      near[C - 1 - x] = R.intra * power(l2, x);
+      near[C - 1 - x] = R.intra * power(l2, x);           // of the steps before, nearest last
       from[x] = R.inter * power(l2, x + 1 - R.shift);
     }
+    if (threadIdx.x < 16) near[C + threadIdx.x] = 0.0f;
   }
   const bool exact = R.sT != nullptr;           // states that the caller sees
   int held = -1;                                // the length that wt and gone are for
   float gone = 0.0f;
-  // outputs: four values of a step, from the lane's column on
-  const int e = e0 + 4 * (lane >> 4);
-  const int64_t start = b * R.os.batch + h * R.os.head + e;
-  auto put = [&](int64_t o, f32x4 v) {
-    if (e + 4 <= R.value) {
-      if (R.o_float) put_any((float*)R.o + o, v);
-      else put_any((T*)R.o + o, v);
-    } else {
+  // Outputs of a chunk go to LDS and from there, whole rows, to memory when the next chunk is being worked on: stores
+  // behind the loads of the next chunk would be waited for with them.
+  const int inner = R.inner, columns = R.value - block * EB < EB ? R.value - block * EB : EB;
+  const int64_t ostep = R.shift ? -R.os.step : R.os.step;
+  const int64_t ofirst = b * R.os.batch + h * R.os.head + block * EB;
+  auto give = [&](int c, int len) {
+    const int64_t base = ofirst + (R.shift ? (int64_t)(n - 1 - c * C) : (int64_t)c * C) * R.os.step;
+    constexpr int PR = EB / 4;
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));               // as above
 #pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        if (e + x >= R.value) continue;
-        if (R.o_float) ((float*)R.o)[o + x] = v[x];
-        else St<T>::st(R.o, o + x, v[x]);
+    for (int x = 0; x < C * PR / NT; ++x) {
+      const int t = tid / PR + x * (NT / PR), e = tid % PR * 4;
+      if (t >= len || e >= columns) continue;
+      const int64_t o = base + t * ostep + e;
+      const f32x4 v = *(const f32x4*)&ot[t * LO + e];
+      if (e + 4 <= columns) {
+        if (R.o_float) put_any((float*)R.o + o, v);
+        else put_any((T*)R.o + o, v);
+      } else {
+#pragma unroll
+        for (int y = 0; y < 3; ++y) {
+          if (e + y >= columns) continue;
+          if (R.o_float) ((float*)R.o)[o + y] = v[y];
+          else St<T>::st(R.o, o + y, v[y]);
+        }
       }
     }
   };
-  const int64_t ostep = R.shift ? -R.os.step : R.os.step;
-  const int64_t orow = start + (R.shift ? (n - 1) * R.os.step : 0) + (lane & 15) * ostep;
   for (int c = c0; c < live; ++c) {
     // addresses in LDS formed anew each time: kept, they cost 60 registers
     int i = lane & 15, g = lane >> 4;
@@ -380,9 +395,9 @@ __global__ __launch_bounds__(64 * NW, lin_occupancy(sizeof(T), KD, NW)) void lin
     const int len = n - c * C < C ? n - c * C : C;
     __syncthreads();                            // the chunk before is done with LDS
     if (threadIdx.x == 0) bad = 0;
-    if (OUT) rq.store(qt);
-    rk.store(kt);
-    rv.store(vt);
+    if (OUT) rq.store(qs);
+    rk.store(ks);
+    rv.store(vs);
     if (held != len) {
       held = len;
       gone = power(l2, len);
@@ -391,6 +406,7 @@ __global__ __launch_bounds__(64 * NW, lin_occupancy(sizeof(T), KD, NW)) void lin
     const bool odd = OUT && rv.lost();
     __syncthreads();
     if (odd) bad = 1;
+    if (OUT && c > c0) give(c - 1, C);
     if (c + 1 < live) load(c + 1);
     // Operands are read from LDS a batch ahead of the products that take them: read and waited for one by one, they
     // made the waits half as long again.
@@ -405,7 +421,7 @@ __global__ __launch_bounds__(64 * NW, lin_occupancy(sizeof(T), KD, NW)) void lin
         f32x4 p = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int k0 = 0; k0 < KD / KS; k0 += B) {
-          if (k0 * KS >= R.inner) continue;
+          if (k0 * KS >= inner) continue;
           Frag<T> kf[B], qf[B];
 #pragma unroll
           for (int kk = 0; kk < B; ++kk) {
@@ -417,13 +433,11 @@ __global__ __launch_bounds__(64 * NW, lin_occupancy(sizeof(T), KD, NW)) void lin
           for (int kk = 0; kk < B; ++kk) mma(kf[kk], qf[kk], p);
         }
         const int apart = t - si * 16 - 4 * g;  // of the first of the lane's four
-        if (ti == si) {
+        float f[4];
 #pragma unroll
-          for (int r = 0; r < 4; ++r) p[r] = apart >= r ? p[r] * near[C - 1 - (apart >= r ? apart - r : 0)] : 0.0f;
-        } else {
+        for (int r = 0; r < 4; ++r) f[r] = near[C - 1 - apart + r];
 #pragma unroll
-          for (int r = 0; r < 4; ++r) p[r] *= near[C - 1 - apart + r];
-        }
+        for (int r = 0; r < 4; ++r) p[r] = apart >= r ? p[r] * f[r] : 0.0f;     // not 0 times what may be NaN
         put4(pt + t * LP + si * 16 + 4 * g, p);
       }
     }
@@ -440,7 +454,7 @@ __global__ __launch_bounds__(64 * NW, lin_occupancy(sizeof(T), KD, NW)) void lin
         queries(0);
 #pragma unroll
         for (int kk = 0; kk < KD / KS; ++kk) {
-          if (kk * KS >= R.inner) continue;
+          if (kk * KS >= inner) continue;
           if (kk + 1 < KD / KS) queries(kk + 1);
           Frag<T> sf;
           state_frag(sf, S, kk);
@@ -501,8 +515,7 @@ __global__ __launch_bounds__(64 * NW, lin_occupancy(sizeof(T), KD, NW)) void lin
     keys(0);
     if constexpr (OUT) {
 #pragma unroll
-      for (int ti = 0; ti < CT; ++ti)
-        if (ti * 16 + i < len) put(orow + (int64_t)(c * C + ti * 16) * ostep, acc[ti]);
+      for (int ti = 0; ti < CT; ++ti) *(f32x4*)&ot[(ti * 16 + i) * LO + w * 16 + 4 * g] = acc[ti];
     }
 #pragma unroll
     for (int dt = 0; dt < KT; ++dt) S[dt] *= gone;
@@ -535,7 +548,7 @@ __global__ __launch_bounds__(64 * NW, lin_occupancy(sizeof(T), KD, NW)) void lin
       }
       if (u + 1 < BATCHES) keys(u + 1);
       phase_end();
-      if (dt * 16 < R.inner) {
+      if (dt * 16 < inner) {
         if constexpr (sizeof(T) == 2) {
 #pragma unroll
           for (int x = 0; x < B; ++x) mma(kf[u & 1][x], part[1], S[dt + x]);
@@ -547,9 +560,16 @@ __global__ __launch_bounds__(64 * NW, lin_occupancy(sizeof(T), KD, NW)) void lin
     }
   }
   if constexpr (OUT) {
+    __syncthreads();
+    if (live > c0) give(live - 1, n - (live - 1) * C < C ? n - (live - 1) * C : C);
+    // steps behind the sequence's end
     const int64_t last = (int64_t)c1 * C < a.length ? (int64_t)c1 * C : a.length;
-    for (int64_t t = (n > c0 * C ? n : c0 * C) + (lane & 15); t < last; t += 16)        // steps behind the sequence's end
-      put(start + t * R.os.step, f32x4{0.0f, 0.0f, 0.0f, 0.0f});
+    for (int64_t t = (n > c0 * C ? n : c0 * C) + w; t < last; t += NW)
+      for (int x = lane; x < columns; x += 64) {
+        const int64_t o = ofirst + t * R.os.step + x;
+        if (R.o_float) ((float*)R.o)[o] = 0.0f;
+        else St<T>::st(R.o, o, 0.0f);
+      }
     if (R.sT != nullptr && seg == a.nseg - 1) {
 #pragma unroll
       for (int dt = 0; dt < KT; ++dt)
@@ -690,20 +710,21 @@ __global__ __launch_bounds__(NT) void linattn_heads_kernel(const float* part_k, 
   }
 }
 
-template <typename T, int KD, int NW>
+template <typename T, int KD, int NW, bool TINY = false>
 int launch_roles(Lin& a, hipStream_t s) {
   const dim3 grid((unsigned)(cdiv64(a.items, 8) * 8 * a.roles * a.most)), threads(64 * NW);
   if (a.nseg > 1) {
-    hipLaunchKernelGGL((linattn_kernel<T, KD, NW, false>), grid, threads, 0, s, a);
+    hipLaunchKernelGGL((linattn_kernel<T, KD, NW, false, TINY>), grid, threads, 0, s, a);
     const unsigned per = (unsigned)(a.most * (NW * (KD / 16) * 64 / NT));
     hipLaunchKernelGGL((linattn_chain_kernel<T, KD, NW>), dim3(per * a.batch * a.heads, a.roles), dim3(NT), 0, s, a);
   }
-  hipLaunchKernelGGL((linattn_kernel<T, KD, NW, true>), grid, threads, 0, s, a);
+  hipLaunchKernelGGL((linattn_kernel<T, KD, NW, true, TINY>), grid, threads, 0, s, a);
   return (int)hipGetLastError();
 }
 
 template <typename T>
 int launch_type(Lin& a, const LinShape& p, hipStream_t s) {
+  if (p.tiny) return launch_roles<T, 256, 8, true>(a, s);
   if (p.pad == 64) return p.waves == 4 ? launch_roles<T, 64, 4>(a, s) : launch_roles<T, 64, 8>(a, s);
   if (p.pad == 128) return p.waves == 4 ? launch_roles<T, 128, 4>(a, s) : launch_roles<T, 128, 8>(a, s);
   return p.waves == 4 ? launch_roles<T, 256, 4>(a, s) : launch_roles<T, 256, 8>(a, s);

@@ -161,7 +161,7 @@ constexpr int64_t LIN_FEW = 256, LIN_MANY = 512;  // workgroups below which sequ
 // How the sums of a direction run: widths summed over padded to `pad`, workgroups of as many waves with 16 value columns
 // each, segments of a sequence.  One shape for all three sums of the backward, which run side by side in a launch.
 struct LinShape {
-  int pad, waves, segments, seg_chunks;
+  int pad, waves, tiny, segments, seg_chunks;
 };
 inline int lin_blocks(const LinShape& p, int64_t value) { return (int)cdiv64(value, 16 * p.waves); }
 inline LinShape lin_shape(const pnn_linattn_desc& d, bool backward) {
@@ -170,6 +170,8 @@ inline LinShape lin_shape(const pnn_linattn_desc& d, bool backward) {
   const int64_t inner = backward ? most : K, value = backward ? most : V;
   p.pad = inner <= 64 ? 64 : inner <= 128 ? 128 : 256;
   p.waves = value <= 64 ? 4 : 8;
+  p.tiny = (K < V ? K : V) * (d.dtype == PNN_F32 ? 4 : 2) < 16;      // rows shorter than a piece: one shape for all
+  if (p.tiny) p.pad = 256, p.waves = 8;
   const int64_t chunks = cdiv64(d.length, LIN_CHUNK);
   const int64_t wgs = d.batch * d.heads * (lin_blocks(p, V) + (backward ? 2 * lin_blocks(p, K) : 0));
   int64_t seg = 1;
