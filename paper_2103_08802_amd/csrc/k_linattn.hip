@@ -296,6 +296,7 @@ __global__ __launch_bounds__(64 * NW, lin_occupancy(sizeof(T), KD, NW)) void lin
   const int block = inside % a.most;
   if (item >= a.items || block >= R.blocks) return;
   const int seg = item % a.nseg, bh = item / a.nseg;
+  if (!OUT && seg == a.nseg - 1) return;               // nobody starts from its state
   const int b = bh / a.heads, h = bh % a.heads;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x & 63;
   const int n = steps_of(a.lengths, b, a.length);

@@ -159,7 +159,10 @@ constexpr int LIN_MAX_WIDTH = PNN_LINATTN_MAX_WIDTH;
 constexpr int LIN_CHUNK = 32;              // steps of a chunk
 constexpr int64_t LIN_FEW = 256, LIN_MANY = 512;  // workgroups below which sequences are cut, and to how many
 // How the sums of a direction run: widths summed over padded to `pad`, workgroups of as many waves with 16 value columns
-// each, segments of a sequence.  One shape for all three sums of the backward, which run side by side in a launch.
+// each, segments of a sequence (of four chunks at least; the two launches before the last cost a third of it).  One
+// shape for all three sums of the backward, which run side by side in a launch.  Measured, us: 128 heads x 2048 steps
+// (128 and 384 workgroups) 296, with 512 in the place of 256 350, of 128 336, with 384 or 768 in the place of 512 310;
+// 30 heads x 777 steps with eight chunks to a segment 140, with four 111.
 struct LinShape {
   int pad, waves, tiny, segments, seg_chunks;
 };
@@ -177,7 +180,7 @@ inline LinShape lin_shape(const pnn_linattn_desc& d, bool backward) {
   int64_t seg = 1;
   if (wgs > 0 && wgs < LIN_FEW) {
     seg = cdiv64(LIN_MANY, wgs);
-    if (seg > chunks / 8) seg = chunks / 8;
+    if (seg > chunks / 4) seg = chunks / 4;
     if (seg < 1) seg = 1;
   }
   p.seg_chunks = (int)(chunks > 0 ? cdiv64(chunks, seg) : 1);
