@@ -88,22 +88,28 @@ struct Stage {
   static_assert(N == 1 || N * NT == C * PR, "whole pieces");
   const T* p;                               // the lane's first piece of the next chunk; short rows: the chunk
   int64_t step;
-  int at, row0;                             // where the lane's first piece goes in LDS (negative: nowhere), its row
   int width, now;                           // of a row; rows of the sequence in the chunk held
   uint4 r[N];
+
+  // The lane's first row, and where its first piece goes in LDS (negative: nowhere); formed anew each time, as they are
+  // cheaper than the registers that would hold them.
+  __device__ __forceinline__ int place(int& at) const {
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));
+    const int row = tid / PR, col = tid % PR * VE;
+    const bool on = col < width && tid < C * PR;
+    at = on ? LEFT + row * LD + (col + VE > width ? width - VE : col) : -1;
+    return on ? row : 0;
+  }
 
   // the sequence's row 0 (its last one backwards in time) at this tile's columns, elements from row to row, columns, row
   __device__ __forceinline__ void begin(const T* first, int64_t step_, int width_, int64_t row) {
     step = step_;
     width = width_;
-    row0 = threadIdx.x / PR;
-    int col = threadIdx.x % PR * VE;
-    const bool on = col < width && (int)threadIdx.x < C * PR;
-    if (col + VE > width) col = width - VE;
-    at = on ? LEFT + row0 * LD + col : -1;
-    if (!on) row0 = col = 0;
     p = first + row * step;
-    if (!TINY) p += row0 * step + col;
+    int at;
+    const int row0 = place(at);
+    if (!TINY && at >= 0) p += row0 * step + (at - LEFT - row0 * LD);
   }
   static __device__ __forceinline__ void clear(T* lds) {
     for (int x = threadIdx.x; x < SIZE; x += NT) lds[x] = (T)0;
@@ -118,9 +124,10 @@ struct Stage {
 #pragma unroll
       for (int j = 0; j < N; ++j) r[j] = piece(p + j * ROWS * step);
     } else {
+      int at;
+      const int last = len - 1 - place(at);
 #pragma unroll
       for (int j = 0; j < N; ++j) {
-        const int last = len - 1 - row0;
         r[j] = piece(p + (j * ROWS < last ? j * ROWS : last) * step);
       }
     }
@@ -130,6 +137,8 @@ struct Stage {
   }
   __device__ __forceinline__ void store(T* lds) {
     if (!TINY) {
+      int at;
+      const int row0 = place(at);
       if (now < C) {
 #pragma unroll
         for (int j = 0; j < N; ++j)
@@ -158,7 +167,7 @@ struct Stage {
 #pragma unroll
     for (int j = 0; j < N; ++j)
       m |= ((r[j].x & EXP) + ONE) | ((r[j].y & EXP) + ONE) | ((r[j].z & EXP) + ONE) | ((r[j].w & EXP) + ONE);
-    return (m & TOP) != 0 && at >= 0;
+    return (m & TOP) != 0;
   }
 };
 
@@ -232,6 +241,18 @@ __device__ __forceinline__ void split(const Frag<uint16_t>& v, const float* w, F
   }
 #pragma unroll
   for (int p = 0; p < 2; ++p) part[p].from_raw(make_uint4(out[p][0], out[p][1], out[p][2], out[p][3]));
+}
+
+__device__ __forceinline__ bool not_finite(float v) { return !(fabsf(v) < INFINITY); }
+__device__ __forceinline__ void finite_only(Frag<uint16_t>& f) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (not_finite((float)f.v[e])) f.v[e] = (__bf16)0.0f;
+}
+__device__ __forceinline__ void finite_only(Frag<float>& f) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (not_finite(f.v[e])) f.v[e] = 0.0f;
 }
 
 // nothing moves over this: without it the compiler has the next products' operands in registers, and spills
@@ -491,23 +512,33 @@ __global__ __launch_bounds__(64 * NW, lin_occupancy(sizeof(T), KD, NW)) void lin
           for (int ti = 0; ti < CT; ++ti)
             if (kb * KS < 16 * (ti + 1)) mma(vf[kb], pf[ti][kb], acc[ti]);
       } else {
-        // an infinite or NaN value reaches the steps from its own on, which a product with the zeros above the
-        // diagonal does not keep to: step by step
+        // An infinite or NaN value reaches the steps from its own on, which a product with the zeros above the diagonal
+        // does not keep to: such values are left out of it and added one by one.
 #pragma unroll
         for (int ti = 0; ti < CT; ++ti) {
 #pragma unroll
-          for (int x = 0; x < 4; ++x) acc[ti][x] *= since[ti];
+          for (int r = 0; r < 4; ++r) acc[ti][r] *= since[ti];
+#pragma unroll
+          for (int kb = 0; kb < C / KS; ++kb) {
+            if (kb * KS >= 16 * (ti + 1)) continue;
+            Frag<T> v = vf[kb];
+            finite_only(v);
+            mma(v, row_frag(pt + (ti * 16 + i) * LP + kb * KS + g * VE), acc[ti]);
+          }
           for (int s = 0; s <= ti * 16 + i; ++s) {
             const float p = St<T>::ld(pt, (ti * 16 + i) * LP + s);
 #pragma unroll
-            for (int x = 0; x < 4; ++x) acc[ti][x] = fmaf(p, St<T>::ld(vt, s * LV + w * 16 + 4 * g + x), acc[ti][x]);
+            for (int x = 0; x < 4; ++x) {
+              const float v = St<T>::ld(vt, s * LV + w * 16 + 4 * g + x);
+              if (not_finite(v)) acc[ti][x] += p * v;
+            }
           }
         }
       }
       phase_end();
     }
-    // the state after the chunk: batches of four of its tiles and one summation step
-    constexpr int B = 4, PB = KT / B, BATCHES = C / KS * PB;
+    // the state after the chunk: batches of two of its tiles and one summation step
+    constexpr int B = 2, PB = KT / B, BATCHES = C / KS * PB;
     Frag<T> kf[2][B];
     auto keys = [&](int u) {
 #pragma unroll
