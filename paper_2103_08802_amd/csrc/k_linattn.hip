@@ -83,37 +83,32 @@ __device__ __forceinline__ int steps_of(const int32_t* lengths, int b, int lengt
 template <typename T, int NT, int W, int PAD, bool TINY>
 struct Stage {
   static constexpr int VE = St<T>::VE, PR = W / VE, N = (C * PR + NT - 1) / NT;
-  static constexpr int LD = W + PAD * VE, LEFT = VE, SIZE = C * LD + LEFT;   // elements: of a row in LDS, in all
+  static constexpr int LD = W + PAD * VE, LEFT = VE, SIZE = LEFT + C * LD;   // elements: of a row in LDS, in all
   static constexpr int ROWS = NT / PR;      // rows that the lanes' first pieces are of
-  static_assert(N == 1 || N * NT == C * PR, "whole pieces");
-  const T* p;                               // the lane's first piece of the next chunk; short rows: the chunk
+  static_assert((N == 1 || N * NT == C * PR) && PAD >= 2, "whole pieces; a place behind the row");
+  const T* p;                               // the lane's first piece of the next chunk; TINY: the chunk
   int64_t step;
+  int at;                                   // where the lane's first piece goes in LDS
   int width, now;                           // of a row; rows of the sequence in the chunk held
   uint4 r[N];
-
-  // The lane's first row, and where its first piece goes in LDS (negative: nowhere); formed anew each time, as they are
-  // cheaper than the registers that would hold them.
-  __device__ __forceinline__ int place(int& at) const {
-    int tid = threadIdx.x;
-    asm volatile("" : "+v"(tid));
-    const int row = tid / PR, col = tid % PR * VE;
-    const bool on = col < width && tid < C * PR;
-    at = on ? LEFT + row * LD + (col + VE > width ? width - VE : col) : -1;
-    return on ? row : 0;
-  }
 
   // the sequence's row 0 (its last one backwards in time) at this tile's columns, elements from row to row, columns, row
   __device__ __forceinline__ void begin(const T* first, int64_t step_, int width_, int64_t row) {
     step = step_;
     width = width_;
     p = first + row * step;
-    int at;
-    const int row0 = place(at);
-    if (!TINY && at >= 0) p += row0 * step + (at - LEFT - row0 * LD);
+    // lanes behind the row's end load its first piece and store it behind the row in LDS, lanes too many row 0's
+    const int row0 = (int)threadIdx.x < C * PR ? threadIdx.x / PR : 0, col = threadIdx.x % PR * VE;
+    const bool on = col < width && (int)threadIdx.x < C * PR;
+    const int to = col + VE > width ? width - VE : col;
+    at = LEFT + row0 * LD + (on ? to : W);
+    if (!TINY) p += row0 * step + (on ? to : 0);
   }
   static __device__ __forceinline__ void clear(T* lds) {
     for (int x = threadIdx.x; x < SIZE; x += NT) lds[x] = (T)0;
   }
+  // the row of the lane's first piece
+  __device__ __forceinline__ int row_at() const { return (at - LEFT + VE) / LD; }
   // The next chunk, of which `len` > 0 rows belong to the sequence.  Nothing here depends on the lane but addresses (a
   // load under a condition waits for the one before it): lanes that store nothing load a piece all the same, and those
   // of rows behind the sequence's end its last row.
@@ -124,12 +119,9 @@ struct Stage {
 #pragma unroll
       for (int j = 0; j < N; ++j) r[j] = piece(p + j * ROWS * step);
     } else {
-      int at;
-      const int last = len - 1 - place(at);
+      const int last = len - 1 - row_at();
 #pragma unroll
-      for (int j = 0; j < N; ++j) {
-        r[j] = piece(p + (j * ROWS < last ? j * ROWS : last) * step);
-      }
+      for (int j = 0; j < N; ++j) r[j] = piece(p + (j * ROWS < last ? j * ROWS : last) * step);
     }
   }
   static __device__ __forceinline__ uint4 piece(const T* s) {
@@ -137,18 +129,16 @@ struct Stage {
   }
   __device__ __forceinline__ void store(T* lds) {
     if (!TINY) {
-      int at;
-      const int row0 = place(at);
       if (now < C) {
+        asm volatile("");                   // a branch, not selections in every chunk
+        const int row0 = row_at();
 #pragma unroll
         for (int j = 0; j < N; ++j)
           if (row0 + j * ROWS >= now) r[j] = make_uint4(0, 0, 0, 0);
       }
-      if (at >= 0) {
-        typedef typename Piece<T>::Mem Mem;
+      typedef typename Piece<T>::Mem Mem;
 #pragma unroll
-        for (int j = 0; j < N; ++j) *(Mem*)(lds + at + j * ROWS * LD) = __builtin_bit_cast(typename Piece<T>::Vec, r[j]);
-      }
+      for (int j = 0; j < N; ++j) *(Mem*)(lds + at + j * ROWS * LD) = __builtin_bit_cast(typename Piece<T>::Vec, r[j]);
     } else {
       for (int x = threadIdx.x; x < C * W; x += NT) {
         const int row = x / W, c = x % W;
@@ -386,29 +376,35 @@ __global__ __launch_bounds__(64 * NW, lin_occupancy(sizeof(T), KD, NW)) void lin
   const int inner = R.inner, columns = R.value - block * EB < EB ? R.value - block * EB : EB;
   const int64_t ostep = R.shift ? -R.os.step : R.os.step;
   const int64_t ofirst = b * R.os.batch + h * R.os.head + block * EB;
-  auto give = [&](int c, int len) {
-    const int64_t base = ofirst + (R.shift ? (int64_t)(n - 1 - c * C) : (int64_t)c * C) * R.os.step;
-    constexpr int PR = EB / 4;
+  constexpr int OR = EB / 4, ON = C * OR / NT;             // pieces of four: of a row, of a lane
+  int64_t oat = ofirst + (R.shift ? (int64_t)(n - 1 - c0 * C) : (int64_t)c0 * C) * R.os.step +
+                (int)(threadIdx.x / OR) * ostep + threadIdx.x % OR * 4;
+  auto give = [&](int len) {
     int tid = threadIdx.x;
     asm volatile("" : "+v"(tid));               // as above
+    const int t = tid / OR, e = tid % OR * 4;
+    const float* const from_lds = &ot[t * LO + e];
+    if (len >= C && columns % 4 == 0) {
+      if (e < columns) {
 #pragma unroll
-    for (int x = 0; x < C * PR / NT; ++x) {
-      const int t = tid / PR + x * (NT / PR), e = tid % PR * 4;
-      if (t >= len || e >= columns) continue;
-      const int64_t o = base + t * ostep + e;
-      const f32x4 v = *(const f32x4*)&ot[t * LO + e];
-      if (e + 4 <= columns) {
-        if (R.o_float) put_any((float*)R.o + o, v);
-        else put_any((T*)R.o + o, v);
-      } else {
-#pragma unroll
-        for (int y = 0; y < 3; ++y) {
-          if (e + y >= columns) continue;
-          if (R.o_float) ((float*)R.o)[o + y] = v[y];
-          else St<T>::st(R.o, o + y, v[y]);
+        for (int x = 0; x < ON; ++x) {
+          const f32x4 v = *(const f32x4*)(from_lds + x * (NT / OR) * LO);
+          if (R.o_float) put_any((float*)R.o + oat + x * (NT / OR) * ostep, v);
+          else put_any((T*)R.o + oat + x * (NT / OR) * ostep, v);
         }
       }
+    } else {
+      asm volatile("");
+      for (int x = 0; x < ON; ++x)
+        for (int y = 0; y < 4; ++y) {
+          if (t + x * (NT / OR) >= len || e + y >= columns) continue;
+          const int64_t o = oat + x * (NT / OR) * ostep + y;
+          const float v = from_lds[x * (NT / OR) * LO + y];
+          if (R.o_float) ((float*)R.o)[o] = v;
+          else St<T>::st(R.o, o, v);
+        }
     }
+    oat += C * ostep;
   };
   for (int c = c0; c < live; ++c) {
     // addresses in LDS formed anew each time: kept, they cost 60 registers
@@ -428,7 +424,7 @@ __global__ __launch_bounds__(64 * NW, lin_occupancy(sizeof(T), KD, NW)) void lin
     const bool odd = OUT && rv.lost();
     __syncthreads();
     if (odd) bad = 1;
-    if (OUT && c > c0) give(c - 1, C);
+    if (OUT && c > c0) give(C);
     if (c + 1 < live) load(c + 1);
     // Operands are read from LDS a batch ahead of the products that take them: read and waited for one by one, they
     // made the waits half as long again.
@@ -593,7 +589,7 @@ __global__ __launch_bounds__(64 * NW, lin_occupancy(sizeof(T), KD, NW)) void lin
   }
   if constexpr (OUT) {
     __syncthreads();
-    if (live > c0) give(live - 1, n - (live - 1) * C < C ? n - (live - 1) * C : C);
+    if (live > c0) give(n - (live - 1) * C);
     // steps behind the sequence's end
     const int64_t last = (int64_t)c1 * C < a.length ? (int64_t)c1 * C : a.length;
     for (int64_t t = (n > c0 * C ? n : c0 * C) + w; t < last; t += NW)
