@@ -162,7 +162,7 @@ constexpr int64_t LIN_FEW = 256, LIN_MANY = 512;  // workgroups below which sequ
 // each, segments of a sequence (of four chunks at least; the two launches before the last cost a third of it).  One
 // shape for all three sums of the backward, which run side by side in a launch.  Measured, us: 128 heads x 2048 steps
 // (128 and 384 workgroups) 296, with 512 in the place of 256 350, of 128 336, with 384 or 768 in the place of 512 310;
-// 30 heads x 777 steps with eight chunks to a segment 140, with four 111.
+// 30 heads x 777 steps with eight chunks to a segment 140, with four 111.  Four waves for 128 heads x 2048 steps: 273 instead of 294.
 struct LinShape {
   int pad, waves, tiny, segments, seg_chunks;
 };
@@ -172,11 +172,17 @@ inline LinShape lin_shape(const pnn_linattn_desc& d, bool backward) {
   const int64_t K = d.key_width, V = d.value_width, most = K > V ? K : V;
   const int64_t inner = backward ? most : K, value = backward ? most : V;
   p.pad = inner <= 64 ? 64 : inner <= 128 ? 128 : 256;
-  p.waves = value <= 64 ? 4 : 8;
   p.tiny = (K < V ? K : V) * (d.dtype == PNN_F32 ? 4 : 2) < 16;      // rows shorter than a piece: one shape for all
-  if (p.tiny) p.pad = 256, p.waves = 8;
+  if (p.tiny) p.pad = 256;
   const int64_t chunks = cdiv64(d.length, LIN_CHUNK);
-  const int64_t wgs = d.batch * d.heads * (lin_blocks(p, V) + (backward ? 2 * lin_blocks(p, K) : 0));
+  auto count = [&](int waves) {
+    p.waves = waves;
+    return d.batch * d.heads * (lin_blocks(p, V) + (backward ? 2 * lin_blocks(p, K) : 0));
+  };
+  // four waves where eight would have idle ones, or where twice the workgroups fill the device more evenly, uncut
+  const int64_t narrow = count(4), wide = count(8);
+  const bool four = !p.tiny && (value <= 64 || (wide < LIN_MANY && narrow >= LIN_FEW));
+  const int64_t wgs = count(four ? 4 : 8);
   int64_t seg = 1;
   if (wgs > 0 && wgs < LIN_FEW) {
     seg = cdiv64(LIN_MANY, wgs);
