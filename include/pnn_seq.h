@@ -31,7 +31,9 @@
  *     PNN_ERR_HIP.  PNN_ERR_TOO_LARGE: sizes or offsets beyond what the kernels index (2^28 samples,
  *     2^22 pieces of 32 tokens x 64 elements, 32 table rows or 16384 elements
  *     of the table, 2^31 - 1 classes, 2^30 steps, 2^21 times 64 channels in a
- *     batch, 2^60 elements from a tensor's first to its last).
+ *     batch, 2^20 heads and 2^30 steps of heads in a batch of linear attention and, where heads share
+ *     keys, 2^32 pieces of four elements of their gradients, 2^30 heads of a norm's rows, 2^60
+ *     elements from a tensor's first to its last).
  */
 #ifndef PNN_SEQ_H
 #define PNN_SEQ_H

@@ -861,8 +861,7 @@ int launch_linattn_bwd(const pnn_linattn_desc& d, const void* q, const void* k, 
   if (const int e = launch_shape(d.dtype, a, w.shape, s)) return e;
   if (shared && d.length > 0) {
     const int64_t rows = d.batch * d.length * d.kv_heads;
-    const int64_t wide = d.key_width > d.value_width ? d.key_width : d.value_width;
-    const dim3 grid((unsigned)cdiv64(rows * cdiv64(wide, 4), NT), 2);
+    const dim3 grid((unsigned)cdiv64(lin_head_threads(d), NT), 2);
 #define HEADS(T) hipLaunchKernelGGL((linattn_heads_kernel<T>), grid, dim3(NT), 0, s, (const float*)(base + w.part_k), \
     (const float*)(base + w.part_v), dk, dv, d.dk, d.dv, rows, (int)d.length, (int)d.kv_heads, group, \
     (int)d.key_width, (int)d.value_width)

@@ -304,6 +304,7 @@ pnn_status pnn_linattn_bwd(const pnn_linattn_desc* d, const void* q, const void*
   if (pnn_status e = heads_ok(d, d->dq, d->heads, d->key_width, true)) return e;
   if (pnn_status e = heads_ok(d, d->dk, d->kv_heads, d->key_width, true)) return e;
   if (pnn_status e = heads_ok(d, d->dv, d->kv_heads, d->value_width, true)) return e;
+  if (lin_head_threads(*d) > (((int64_t)1 << 32) - 256)) return PNN_ERR_TOO_LARGE;
   if (d->batch == 0) return PNN_OK;
   if (log_decay == nullptr ||
       (d->length > 0 && (q == nullptr || k == nullptr || v == nullptr || dout == nullptr || dq == nullptr ||
@@ -393,7 +394,9 @@ pnn_status pnn_norm_bwd(const pnn_norm_desc* d, const void* x, const float* w_po
     for (int j = 0; j < i; ++j)
       if (tensors[i].p != nullptr && tensors[i].p == tensors[j].p && !(i == 7 && j == 4 && same(d->dres, d->dh, d)))
         return PNN_ERR_SHAPE;
-  if (dw_post != nullptr && dw_post == dw_pre) return PNN_ERR_SHAPE;
+  const float* const dw[2] = {dw_post, dw_pre};
+  for (int i = 0; i < 2; ++i)
+    if (dw[i] != nullptr && (dw[i] == dw[1 - i] || dw[i] == w_post || dw[i] == w_pre)) return PNN_ERR_SHAPE;
   return launch_norm_bwd(*d, x, w_post, gate, res, w_pre, dy, dh, dx, dgate, dres, dw_post, dw_pre, accumulate, workspace,
                          (hipStream_t)stream)
              ? PNN_ERR_HIP
@@ -425,6 +428,8 @@ pnn_status pnn_policy_fwd_bwd(const pnn_policy_desc* d, const void* logits, cons
     return PNN_ERR_ALIGN;
   if (dlogits == logits && d->rows > 1 && d->grad_stride != d->logit_stride) return PNN_ERR_SHAPE;
   if (loss == logp) return PNN_ERR_SHAPE;
+  for (const float* in : {advantage, old, ref, weight})
+    if (in != nullptr && (loss == in || logp == in)) return PNN_ERR_SHAPE;
   return launch_policy(*d, logits, tokens, advantage, old, ref, weight, loss, logp, dlogits, (hipStream_t)stream)
              ? PNN_ERR_HIP
              : PNN_OK;

@@ -226,6 +226,11 @@ inline LinBwd lin_bwd(const pnn_linattn_desc& d) {
   w.bytes = o;
   return w;
 }
+// threads of the kernel that adds up what heads share: four elements each
+inline int64_t lin_head_threads(const pnn_linattn_desc& d) {
+  const int64_t wide = d.key_width > d.value_width ? d.key_width : d.value_width;
+  return d.heads > d.kv_heads ? d.batch * d.length * d.kv_heads * cdiv64(wide, 4) : 0;
+}
 int launch_linattn_fwd(const pnn_linattn_desc& d, const void* q, const void* k, const void* v, const float* decay,
                        const int32_t* lengths, const float* s0, void* o, float* sT, void* ws, hipStream_t s);
 int launch_linattn_bwd(const pnn_linattn_desc& d, const void* q, const void* k, const void* v, const float* decay,

@@ -119,6 +119,15 @@ def test_linattn_arguments(L):
     assert _lb(L, _lin(batch=0), q=None, dq=None, log_decay=None, ws=None) == 0
 
 
+def test_linattn_shared_gradients_too_large(L):
+    """The gradients of shared keys and values are added up by a thread for four elements: 2^32 at most in a launch."""
+    row = Q.HeadStride(0, 1 << 10, 256)
+    for length, st in ((1 << 26, LARGE), ((1 << 26) - 256, NULL)):
+        d = _lin(batch=1, length=length, heads=2, kv_heads=1, key_width=256,
+                 **{n: row for n in ("q", "k", "v", "o", "dout", "dq", "dk", "dv")})
+        assert _lb(L, d, log_decay=None) == st
+
+
 # ---- norms -------------------------------------------------------------------------------------
 
 def _norm(**kw):
@@ -190,6 +199,12 @@ def test_norm_arguments(L):
     assert _nb(L, d, x=None, dx=None, dgate=None, dres=None, dw_post=None, dw_pre=None) == 0
 
 
+def test_norm_weight_gradients_in_place_of_weights(L):
+    for k in ("dw_post", "dw_pre"):
+        for w in ("w_post", "w_pre"):
+            assert _nb(L, _norm(), **{k: NBWD[w]}) == SHAPE, (k, w)
+
+
 # ---- policy loss -------------------------------------------------------------------------------
 
 def _policy(**kw):
@@ -226,6 +241,12 @@ def test_policy_arguments(L):
     assert _pol(L, _policy(grad_stride=40), dz=POL["z"]) == SHAPE
     assert _pol(L, d, logp=POL["loss"]) == SHAPE
     assert _pol(L, _policy(rows=0), z=None, loss=None) == 0
+
+
+def test_policy_outputs_in_place_of_inputs(L):
+    for k in ("loss", "logp"):
+        for o in ("advantage", "old", "ref", "weight"):
+            assert _pol(L, _policy(), **{k: POL[o]}) == SHAPE, (k, o)
 
 
 def test_python_descriptions():
