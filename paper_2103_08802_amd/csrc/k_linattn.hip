@@ -4,10 +4,11 @@
 // Chunks of C steps.  With i, j steps of a chunk of len and S the state before it,
 //   o_i = scale (sum_{j <= i} lambda^(i - j) (q_i k_j) v_j + lambda^(i + 1) q_i S)
 //   S  <- lambda^len S + sum_j k_j (lambda^(len - 1 - j) v_j)^T,
-// four products on the matrix units.  A workgroup of four waves takes 64 ET value columns of a head through the
-// chunks; a wave holds the state of its 16 ET columns in registers, in the layout that the products leave it in and
+// four products on the matrix units.  A workgroup of four or eight waves takes 64 or 128 value columns of a head through
+// the chunks; a wave holds the state of its 16 columns in registers, in the layout that the products leave it in and
 // that they take it in (a state column's rows are the summation index of q S, so its registers are an operand as they
-// stand).  q k is formed once a workgroup and goes through LDS.
+// stand).  q k is formed once a workgroup and goes through LDS.  32 steps to a chunk, so that q, k, v and the outputs
+// fit LDS for three workgroups a CU (64 steps with two column tiles a wave: 477 us where this took 384).
 //
 // The backward is the same sum three times:
 //   dq: queries do, keys v, values k, from the transposed state;
@@ -16,6 +17,13 @@
 //
 // Few heads do not fill the device: their sequences are cut into segments, whose states from zero are formed by a
 // first launch (without outputs), chained by a second, and taken as first states by the third.
+//
+// What bounds it is a chunk's chain of waits (copy to LDS, barrier, q k, barrier, outputs, state), not the matrix units
+// or memory.  8 sequences of 2048 steps, 16 heads of 128 x 128, bf16: forward 107 us (270 MB, 2.5 TB/s, one workgroup
+// of four waves a CU, 1.7 us a chunk), backward 167 us (700 MB, 4.2 TB/s, three a CU, 2.6 us a chunk); without its
+// products the forward takes 78, without products and output stores 44.  One sequence of 32768 steps: 73 us for the
+// states (293 MB, 4.0 TB/s), 16 for the chain, 136 for the outputs (577 MB, 4.2 TB/s).  A chunk's products with all
+// operands read ahead, more registers and fewer waves: no gain (107, backward 166), spills in the eight-wave form.
 //
 // Roundings to bf16 besides the outputs' (bf16 tensors only): the weighted q k and the state, where they are operands
 // of the products with v and q; each is as large as the output's own rounding.  The state itself is fp32, and the
@@ -380,7 +388,7 @@ __global__ __launch_bounds__(64 * NW, lin_occupancy(sizeof(T), KD, NW)) void lin
                 (int)(threadIdx.x / OR) * ostep + threadIdx.x % OR * 4;
   auto give = [&](int len) {
     int tid = threadIdx.x;
-    asm volatile("" : "+v"(tid));               // as above
+    asm volatile("" : "+v"(tid));               // formed anew in each chunk, as the addresses below
     const int t = tid / OR, e = tid % OR * 4;
     const float* const from_lds = &ot[t * LO + e];
     if (len >= C && columns % 4 == 0) {

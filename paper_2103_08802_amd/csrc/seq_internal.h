@@ -162,7 +162,8 @@ constexpr int64_t LIN_FEW = 256, LIN_MANY = 512;  // workgroups below which sequ
 // each, segments of a sequence (of four chunks at least; the two launches before the last cost a third of it).  One
 // shape for all three sums of the backward, which run side by side in a launch.  Measured, us: 128 heads x 2048 steps
 // (128 and 384 workgroups) 296, with 512 in the place of 256 350, of 128 336, with 384 or 768 in the place of 512 310;
-// 30 heads x 777 steps with eight chunks to a segment 140, with four 111.  Four waves for 128 heads x 2048 steps: 273 instead of 294.
+// 30 heads x 777 steps with eight chunks to a segment 140, with four 111.  Four waves to a workgroup: 128 heads x 2048
+// steps 273, with eight 294.
 struct LinShape {
   int pad, waves, tiny, segments, seg_chunks;
 };
