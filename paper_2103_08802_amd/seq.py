@@ -4,8 +4,8 @@ recurrence, linear attention, norms, distillation and policy loss.
 Every ``pnn_*`` function has the name of the C entry point it calls and takes a description, device
 pointers as Python ints or objects with ``data_ptr()`` (None: NULL) and a stream.  ``embed_desc``,
 ``scan_desc``, ``distill_desc``, ``linattn_desc``, ``norm_desc`` and ``policy_desc`` fill the descriptions from
-tensors; fill one once and use it for every call on tensors of the same types, shapes and strides.  As in ``binding``, nothing falls back to anything
-else: a refused call raises ``PnnError``.
+tensors; fill one once and use it for every call on tensors of the same types, shapes and strides.  As in
+``binding``, nothing falls back to anything else: a refused call raises ``PnnError``.
 """
 from __future__ import annotations
 
