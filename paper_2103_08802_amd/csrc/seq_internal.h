@@ -239,13 +239,14 @@ int launch_linattn_bwd(const pnn_linattn_desc& d, const void* q, const void* k, 
                        void* dv, float* ds0, void* ws, hipStream_t s);
 
 // ---- norms ----
-// How rows run: lanes and 16-byte pieces a lane of one, workgroups of the forward and the backward
+// How rows run: lanes and 16-byte pieces a lane of one, whether their end cuts a piece, workgroups of the forward and
+// the backward
 struct NormShape {
-  int lanes, pieces, forward, backward;
+  int lanes, pieces, tail, forward, backward;
 };
 // waves of the backward that registers leave room for on a SIMD, with as many elements a lane
-constexpr int norm_waves(int lanes, int elements) {
-  return lanes == 1024 ? 4 : elements <= 4 ? 7 : elements <= 8 ? 5 : 3;
+constexpr int norm_waves(int lanes, int elements, bool tail) {
+  return lanes == 1024 ? 4 : elements <= 4 ? 7 - tail : elements <= 8 ? 5 - tail : 3 - tail;
 }
 inline NormShape norm_shape(const pnn_norm_desc& d) {
   NormShape p;
@@ -253,11 +254,12 @@ inline NormShape norm_shape(const pnn_norm_desc& d) {
   const int64_t n = cdiv64(d.width, ve), rows = d.rows * d.heads;
   p.lanes = n <= 32 ? 16 : n <= 128 ? 64 : n <= 512 ? 256 : 1024;
   p.pieces = n <= p.lanes ? 1 : n <= 2 * p.lanes ? 2 : 4;
+  p.tail = d.width % ve != 0;
   const int64_t teams = p.lanes < 256 ? 256 / p.lanes : 1, wgs = cdiv64(rows, teams);
   // As many workgroups as run at a time: 16384 x 2048 backward with 1280 (five a CU) 86 us, with 1536 113.  The forward
   // likes fewer than that: 50 us with 1024, 57 with 2048; 16-lane rows 37 with 1536, 39 with 1024.
   const int64_t most_f = p.lanes == 1024 ? 512 : p.lanes == 256 ? 1024 : 1536;
-  const int64_t most_b = p.lanes == 1024 ? 256 : 256 * norm_waves(p.lanes, p.pieces * ve);
+  const int64_t most_b = p.lanes == 1024 ? 256 : 256 * norm_waves(p.lanes, p.pieces * ve, p.tail);
   p.forward = (int)(wgs < most_f ? wgs : most_f);
   p.backward = (int)(wgs < most_b ? wgs : most_b);
   return p;
