@@ -8,9 +8,9 @@
 // LDS, workgroups by a second launch, each in a fixed order.  The sums that a row needs go over DPP, and over LDS where
 // a row has more than a wave.
 //
-// Bound by memory.  bf16, 16384 rows of 2048 with a residual: forward 53 us (269 MB, 5.1 TB/s), backward 84 us (424 MB,
+// Bound by memory.  bf16, 16384 rows of 2048 with a residual: forward 52 us (269 MB, 5.1 TB/s), backward 85 us (424 MB,
 // 5.0 TB/s, 21 MB of it partial weight gradients) and 8.5 us to join these.  262144 heads of 128 with a gate: forward 38
-// us (201 MB, 5.3 TB/s), backward 61 us (336 MB, 5.5 TB/s) and 5.  Rows are loaded when their turn comes: a row ahead in
+// us (201 MB, 5.3 TB/s), backward 58 us (336 MB, 5.8 TB/s) and 5.  Rows are loaded when their turn comes: a row ahead in
 // registers costs a wave a SIMD and gained nothing.  Stores of tensors larger than L2 go past it (heads' backward 107 us
 // if they do not).
 #include "device_common.h"
