@@ -211,10 +211,11 @@ typedef struct {
   int64_t width;           /* 1 .. PNN_NORM_MAX_WIDTH */
   int post;                /* != 0: norm of the block's output x */
   int pre;                 /* != 0: norm of the sum h, the next block's input */
-  pnn_row_stride x, gate, res, h, y;          /* forward (backward: x, gate, res) */
+  pnn_row_stride x, gate, res, h, y;          /* forward (backward: x, gate and res or h) */
   pnn_row_stride dy, dh, dx, dgate, dres;     /* backward */
   float eps;               /* > 0 */
   float alpha;             /* scale of the block's output in the sum */
+  int stored;              /* backward with pre: != 0: res is h as the forward stored it, 0: the residual */
 } pnn_norm_desc;
 
 #define PNN_NORM_MAX_WIDTH 16384
@@ -222,7 +223,7 @@ typedef struct {
 /* With norm(u) = u / sqrt(mean(u^2) + eps) over the width:
  *     a = post ? w_post norm(x) : x,   h = res + alpha a silu(gate),   y = w_pre norm(h)   (pre != 0)
  * w_post, w_pre: float[width], the same for every head (NULL: ones).  gate, res (NULL: without), h (NULL: not wanted,
- * with pre; may be res itself, with the same strides), y (needed if pre != 0, not looked at otherwise).  y is formed from the sum
+ * with pre; may be res itself, with the same strides: the backward then takes it with `stored`), y (needed if pre != 0, not looked at otherwise).  y is formed from the sum
  * before it is rounded to h.  silu(-inf) is 0.  A row whose squares pass the float range is normed to zeros. */
 pnn_status pnn_norm_fwd(const pnn_norm_desc* d, const void* x, const float* w_post, const void* gate, const void* res,
                         const float* w_pre, void* h, void* y, void* stream);
@@ -230,11 +231,14 @@ pnn_status pnn_norm_fwd(const pnn_norm_desc* d, const void* x, const float* w_po
 /* Bytes of workspace for pnn_norm_bwd (needed if dw_post or dw_pre is wanted). */
 pnn_status pnn_norm_workspace_size(const pnn_norm_desc* d, size_t* bytes);
 
-/* The gradients, from dy (pre != 0) and (nullable) dh, the gradient that reaches h otherwise.  x, gate, res, w_post, w_pre
- * as in the forward, whose h is formed again without its rounding (x is not looked at without post, pre and gate, res
- * not without pre).  dres = dL/dres (nullable; may be dh itself, with the same strides), dx, dgate (nullable).  dw_post,
- * dw_pre (float[width], nullable): overwritten, or added to with accumulate != 0; each sum has one order.  Without dres,
- * dx, dgate and both weights' gradients nothing is done. */
+/* The gradients, from dy (pre != 0) and (nullable) dh, the gradient that reaches h otherwise.  x, gate, w_post, w_pre as
+ * in the forward.  res (looked at with pre only): the residual as in the forward (NULL: without), from which h is formed
+ * again without its rounding, or, with `stored`, h as the forward stored it (h's strides; after a forward in place there
+ * is nothing else): the gradients then are those at the stored h, whose rounding to bf16 is about 2e-3 of the weights'
+ * gradients.  x is not looked at without post and gate where h is stored or pre is 0.  dres = dL/dres (nullable; may be
+ * dh itself, with the same strides), dx, dgate (nullable).  dw_post, dw_pre (float[width], nullable): overwritten, or
+ * added to with accumulate != 0; each sum has one order.  Without dres, dx, dgate and both weights' gradients nothing is
+ * done. */
 pnn_status pnn_norm_bwd(const pnn_norm_desc* d, const void* x, const float* w_post, const void* gate, const void* res,
                         const float* w_pre, const void* dy, const void* dh, void* dx, void* dgate, void* dres,
                         float* dw_post, float* dw_pre, int accumulate, void* workspace, void* stream);

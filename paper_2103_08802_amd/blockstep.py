@@ -94,7 +94,7 @@ class BlockModel:
         h, y, b = r["h"][0], r["y"][0], r["b"][0]
         r["first"] = Q.norm_desc(h, y=y, dy=r["dy"], dh=r["dh"], dx=r["db"], pre=True, eps=self.EPS)
         r["sum"] = Q.norm_desc(b, res=h, h=h, y=y, dy=r["dy"], dh=r["dh"], dx=r["db"], dres=r["dh"], pre=True,
-                               eps=self.EPS, alpha=self.alpha)
+                               eps=self.EPS, alpha=self.alpha, stored=False)
         return r
 
     def split(self, p):

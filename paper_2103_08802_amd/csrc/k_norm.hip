@@ -30,7 +30,7 @@ struct Norm {
   float* part;                    // [workgroups][2][width]: partial gradients of w_post and w_pre
   pnn_row_stride xs, gs, rs, hs, ys, dys, dhs, dxs, dgs, drs;
   int total, heads, width;        // rows x heads, heads, elements of a row
-  int post, pre, dw_post, dw_pre, past;
+  int post, pre, stored, dw_post, dw_pre, past;     // stored: res is h, as the forward stored it
   float eps, alpha, inv_width;
 };
 
@@ -307,13 +307,15 @@ __global__ __launch_bounds__(TL < 256 ? 256 : TL, norm_waves(TL, NP * St<T>::VE,
     }
     float w[N];
     if (a.pre) {
-      if (a.post) weight(0, w);
-      // h as the forward formed it, before its rounding
+      if (!a.stored) {
+        if (a.post) weight(0, w);
+        // h as the forward formed it, before its rounding
 #pragma unroll
-      for (int e = 0; e < N; ++e) {
-        float n = a.post ? x[e] * r1 * w[e] : x[e];
-        if (GATE) n *= silu(g[e], sigmoid(g[e]));
-        h[e] = a.res != nullptr ? fmaf(a.alpha, n, h[e]) : a.alpha * n;
+        for (int e = 0; e < N; ++e) {
+          float n = a.post ? x[e] * r1 * w[e] : x[e];
+          if (GATE) n *= silu(g[e], sigmoid(g[e]));
+          h[e] = a.res != nullptr ? fmaf(a.alpha, n, h[e]) : a.alpha * n;
+        }
       }
       float s[2] = {0.0f, 0.0f};
       weight(1, w);
@@ -464,6 +466,8 @@ int launch_norm_bwd(const pnn_norm_desc& d, const void* x, const float* w_post, 
   Norm a = common(d);
   a.x = x, a.w_post = w_post, a.gate = gate, a.res = res, a.w_pre = w_pre, a.dy = dy, a.dh = dh;
   a.dx = dx, a.dgate = dgate, a.dres = dres;
+  a.stored = d.pre && d.stored;
+  if (a.stored) a.rs = d.h;
   a.part = (float*)ws;
   a.dw_post = dw_post != nullptr;
   a.dw_pre = dw_pre != nullptr;

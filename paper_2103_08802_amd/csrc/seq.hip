@@ -370,19 +370,20 @@ pnn_status pnn_norm_bwd(const pnn_norm_desc* d, const void* x, const float* w_po
   if (!d->pre) res = dy = nullptr, dw_pre = nullptr;
   if (!d->post) dw_post = nullptr;
   if (gate == nullptr) dgate = nullptr;
-  const bool needs_x = d->post || d->pre || gate != nullptr;
+  const bool stored = d->pre && d->stored, needs_x = d->post || (d->pre && !stored) || gate != nullptr;
   if (!needs_x) x = nullptr;
   const struct {
     const void* p;
     const pnn_row_stride& s;
     bool out;
-  } tensors[8] = {{x, d->x, false},   {gate, d->gate, false}, {res, d->res, false}, {dy, d->dy, false},
+  } tensors[8] = {{x, d->x, false},   {gate, d->gate, false}, {res, stored ? d->h : d->res, false}, {dy, d->dy, false},
                   {dh, d->dh, false}, {dx, d->dx, true},      {dgate, d->dgate, true}, {dres, d->dres, true}};
   for (const auto& t : tensors)
     if (t.p != nullptr)
       if (pnn_status e = norm_rows_ok(d, t.s, t.out)) return e;
   if (dx == nullptr && dgate == nullptr && dres == nullptr && dw_post == nullptr && dw_pre == nullptr) return PNN_OK;
-  if (d->rows > 0 && ((needs_x && x == nullptr) || (d->pre && dy == nullptr))) return PNN_ERR_NULL;
+  if (d->rows > 0 && ((needs_x && x == nullptr) || (d->pre && dy == nullptr) || (stored && res == nullptr)))
+    return PNN_ERR_NULL;
   if (d->rows > 0 && (dw_post != nullptr || dw_pre != nullptr) && workspace == nullptr) return PNN_ERR_NULL;
   const int es = type_size(d->dtype);
   for (const auto& t : tensors)

@@ -10,6 +10,7 @@ tensors; fill one once and use it for every call on tensors of the same types, s
 from __future__ import annotations
 
 import ctypes
+import weakref
 
 from . import binding
 from .binding import PNN_BF16, PNN_F32, PnnError  # noqa: F401
@@ -62,7 +63,8 @@ class RowStride(ctypes.Structure):
 class NormDesc(ctypes.Structure):
     _fields_ = [("dtype", _i), ("rows", _i64), ("heads", _i64), ("width", _i64), ("post", _i), ("pre", _i)] + \
                [(n, RowStride) for n in ("x", "gate", "res", "h", "y", "dy", "dh", "dx", "dgate", "dres")] + \
-               [("eps", _f), ("alpha", _f)]
+               [("eps", _f), ("alpha", _f), ("stored", _i)]
+    sum = kept = None        # norm_desc: what pnn_norm_bwd knows the described h by, and (the residual it takes instead)
 
 
 class PolicyDesc(ctypes.Structure):
@@ -191,11 +193,19 @@ def linattn_desc(q, k, v, o, dout=None, dq=None, dk=None, dv=None, scale=1.0):
 
 
 def norm_desc(x, gate=None, res=None, h=None, y=None, dy=None, dh=None, dx=None, dgate=None, dres=None, post=False,
-              pre=False, eps=1e-5, alpha=1.0):
+              pre=False, eps=1e-5, alpha=1.0, stored=None, kept=False):
     """Tensors [rows][heads][width], or [rows][width] for one head, with contiguous widths, all of x's type and shape; those
-    that no call uses may be left out.  ``post``: norm of x, ``pre``: norm of h."""
+    that no call uses may be left out.  ``post``: norm of x, ``pre``: norm of h.
+
+    ``stored``: whether the ``res`` that pnn_norm_bwd gets is h as the forward stored it (True; the form after a forward in
+    place) or the residual (False).  Left out it is the residual, and the call refuses the tensor described as h, which
+    may be either.  ``kept``: what h is the sum of stays as it is until the backward, which, given the tensor
+    described as h, forms it again from x, gate and the tensor described as res, without its rounding; such a description
+    holds that tensor and serves its own tensors only."""
     if x.dim() not in (2, 3):
         raise ValueError(f"x: [rows][heads][width] or [rows][width] expected, not {tuple(x.shape)}")
+    if kept and (stored or h is None or (res is not None and res.data_ptr() == h.data_ptr() != 0)):
+        raise ValueError("kept: h, apart from res, and a sum that the backward forms again")
     dt, shape = _dtype(x), tuple(x.shape)
     st = []
     for n, t in (("x", x), ("gate", gate), ("res", res), ("h", h), ("y", y), ("dy", dy), ("dh", dh), ("dx", dx),
@@ -206,8 +216,13 @@ def norm_desc(x, gate=None, res=None, h=None, y=None, dy=None, dh=None, dx=None,
         if tuple(t.shape) != shape or _dtype(t) != dt or (shape[-1] > 1 and t.stride(-1) != 1):
             raise ValueError(f"{n}: shape {tuple(t.shape)}, {t.dtype}, strides {tuple(t.stride())} do not fit")
         st.append(RowStride(t.stride(0), t.stride(1) if len(shape) == 3 else shape[-1]))
-    return NormDesc(dt, shape[0], shape[1] if len(shape) == 3 else 1, shape[-1], int(bool(post)), int(bool(pre)), *st,
-                    eps, alpha)
+    d = NormDesc(dt, shape[0], shape[1] if len(shape) == 3 else 1, shape[-1], int(bool(post)), int(bool(pre)), *st,
+                 eps, alpha, int(bool(stored)))
+    if kept or (stored is None and h is not None):
+        d.sum = weakref.ref(h)
+    if kept:
+        d.kept = (res,)
+    return d
 
 
 def policy_desc(logits, dlogits=None, temperature=1.0, clip_low=0.2, clip_high=0.2, kl=0.0, scale=1.0):
@@ -291,7 +306,24 @@ def pnn_norm_workspace_size(desc):
     return v.value
 
 
+def _norm_sum(desc, res):
+    """What stands in res's place in the backward: the residual or, if the description says so, h."""
+    if desc.sum is None or res is None or not desc.pre:
+        return res
+    h, at = desc.sum(), _ptr(res)
+    is_h = h is not None and at == h.data_ptr() != 0
+    if desc.kept is None:
+        if is_h:
+            raise ValueError("res is the tensor described as h: norm_desc's stored says whether it is the sum here")
+        return res
+    if not is_h and at != _ptr(desc.kept[0]):
+        raise ValueError("res: a description with kept serves its own tensors only")
+    return desc.kept[0]
+
+
 def pnn_norm_bwd(desc, x, w_post, gate, res, w_pre, dy, dh, dx, dgate, dres, dw_post, dw_pre, accumulate, workspace, stream):
+    """``res``: the residual, or h (norm_desc's ``stored`` and ``kept``)."""
+    res = _norm_sum(desc, res)
     _check(lib().pnn_norm_bwd(desc, _ptr(x), _ptr(w_post), _ptr(gate), _ptr(res), _ptr(w_pre), _ptr(dy), _ptr(dh), _ptr(dx),
                               _ptr(dgate), _ptr(dres), _ptr(dw_post), _ptr(dw_pre), int(bool(accumulate)),
                               _ptr(workspace), stream), "pnn_norm_bwd")
