@@ -399,7 +399,7 @@ def run(state):
     seq.pnn_norm_fwd(s["desc"], s["x"], s["w1"], s["gate"], s["res"], s["w2"], s["h"], s["y"], stream)
     out = [s["h"], s["y"]]
     if kind == "norm_train":
-        seq.pnn_norm_bwd(s["desc"], s["x"], s["w1"], s["gate"], s["res"], s["w2"], s["dy"], s["dh"], s["dx"], s["dgate"],
+        seq.pnn_norm_bwd(s["desc"], s["x"], s["w1"], s["gate"], s["h"], s["w2"], s["dy"], s["dh"], s["dx"], s["dgate"],
                          s["dres"], s["dw1"], s["dw2"], False, s["ws"], stream)
         out += [s["dx"], s["dgate"], s["dres"], s["dw2"], s["dw1"]]
     return [t for t in out if t is not None]
