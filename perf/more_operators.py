@@ -181,7 +181,7 @@ def _prepare_norm(c, g):
         from paper_2103_08802_amd import seq
         more = {n: s[n] for n in ("dy", "dh", "dx", "dgate", "dres")} if train else {}
         s["desc"] = seq.norm_desc(s["x"], gate=s["gate"], res=s["res"], h=s["h"], y=s["y"], **more, post=c["post"],
-                                  pre=c["pre"], eps=EPS, alpha=s["alpha"])
+                                  pre=c["pre"], eps=EPS, alpha=s["alpha"], kept=train)
         if train:
             s["ws"] = torch.empty(max(seq.pnn_norm_workspace_size(s["desc"]), 256), device=DEV, dtype=torch.uint8)
     return s
