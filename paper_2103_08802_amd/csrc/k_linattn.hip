@@ -104,13 +104,10 @@ struct Stage {
   __device__ __forceinline__ void begin(const T* first, int64_t step_, int width_, int64_t row) {
     step = step_;
     width = width_;
+    const LinPiece x = lin_piece(threadIdx.x, C, PR, VE, width);
+    at = LEFT + x.row * LD + x.to;
     p = first + row * step;
-    // lanes behind the row's end load its first piece and store it behind the row in LDS, lanes too many row 0's
-    const int row0 = (int)threadIdx.x < C * PR ? threadIdx.x / PR : 0, col = threadIdx.x % PR * VE;
-    const bool on = col < width && (int)threadIdx.x < C * PR;
-    const int to = col + VE > width ? width - VE : col;
-    at = LEFT + row0 * LD + (on ? to : W);
-    if (!TINY) p += row0 * step + (on ? to : 0);
+    if (!TINY) p += x.row * step + x.from;
   }
   static __device__ __forceinline__ void clear(T* lds) {
     for (int x = threadIdx.x; x < SIZE; x += NT) lds[x] = (T)0;

@@ -167,6 +167,21 @@ constexpr int64_t LIN_FEW = 256, LIN_MANY = 512;  // workgroups below which sequ
 struct LinShape {
   int pad, waves, tiny, segments, seg_chunks;
 };
+// Where a lane's first 16-byte piece of a tile of rows is: `pieces` to a row, `ve` elements each, `width` elements of a row
+// from the tile's first column to the row's end, which may be behind the tile's.  The piece that the row's end cuts is
+// moved back to end there, in front of the tile's columns if need be: a row is at least a piece long.  Lanes with nothing
+// to load (behind the row's end; behind the tile's `rows`) load the row's first piece, likewise, and store it behind
+// the tile's columns.
+struct LinPiece {
+  int row, from, to;                       // row, first element in memory and in LDS
+};
+__host__ __device__ constexpr LinPiece lin_piece(int lane, int rows, int pieces, int ve, int width) {
+  const bool there = lane < rows * pieces;
+  const int col = lane % pieces * ve, last = width - ve, first = last < 0 ? last : 0;
+  const bool on = there && col < width;
+  const int at = col < last ? col : last;
+  return LinPiece{there ? lane / pieces : 0, on ? at : first, on ? at : pieces * ve};
+}
 inline int lin_blocks(const LinShape& p, int64_t value) { return (int)cdiv64(value, 16 * p.waves); }
 inline LinShape lin_shape(const pnn_linattn_desc& d, bool backward) {
   LinShape p;
