@@ -130,11 +130,13 @@ class BlockModel:
 
     def load(self, tokens, answers, advantage=None, old=None, ref=None):
         """tokens [batch][length]; per position: the token that was drawn from its logits (below 0: none), its advantage,
-        and its log probability when it was drawn and of the reference."""
+        and its log probability when it was drawn and of the reference (zeros where they are left out)."""
         self.tokens.copy_(tokens.view_as(self.tokens))
         self.answers.copy_(answers.reshape(-1))
         for dst, src in ((self.advantage, advantage), (self.old, old), (self.ref, ref)):
-            if src is not None:
+            if src is None:
+                dst.zero_()
+            else:
                 dst.copy_(src.reshape(-1))
 
     def log_probabilities(self, lengths=None):
