@@ -197,9 +197,11 @@ class BlockModel:
 
     def answer(self, tokens, noise, lengths=None):
         """Continues prompts [batch][length] (of ``lengths`` tokens, int32) by as many tokens as noise
-        [steps][batch][vocab] has."""
+        [steps][batch][vocab] has.  A prompt of no tokens has no logits: its first answer is drawn uniformly."""
         t = self.torch
         self.tokens.copy_(tokens.view_as(self.tokens))
+        if lengths is not None:                              # what is behind a prompt's end is padding, whatever it holds
+            self.tokens.masked_fill_(t.arange(self.length, device=self.dev) >= lengths[:, None], -1)
         logits = self.forward(lengths, keep=self.states).view(self.batch, self.length, -1)
         if lengths is None:
             last = logits[:, -1]
