@@ -261,7 +261,8 @@ typedef struct {
  *     loss = -min(r A, clip(r, 1 - clip_low, 1 + clip_high) A) + kl (exp(x) - 1 - x),   A = advantage
  *     dlogits_v = scale weight c / tau ([v = a] - p_v),   c = -[r A <= clip(r) A] r A - kl (exp(x) - 1)
  * logp (nullable): float[rows], l.  old (NULL: r = 1, with the gradient of r at 1), ref, weight (NULL: ones): float[rows].
- * The weight is a factor of the row's gradient, not of its loss.  A row with a token below 0 (a prompt's, padding)
+ * The weight is a factor of the row's gradient, not of its loss.  r is infinite past the float range; with an advantage of
+ * 0 there is no policy term all the same.  A row with a token below 0 (a prompt's, padding)
  * has loss, l and gradient 0 whatever the rest of it holds; a token not below `classes` makes them NaN.
  * loss: float[rows].  dlogits (nullable: loss and logp only) may be logits itself (with the same stride).
  * PNN_ERR_VALUE: tau not above zero, a clip bound below zero, or tau, log2(e) / tau, a bound, kl, scale or scale / tau

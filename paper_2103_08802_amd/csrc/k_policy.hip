@@ -135,7 +135,7 @@ __global__ __launch_bounds__(NT, NC == 8 ? 8 : 1) void policy_kernel(Policy a) {
   for (int x = 0; x < NWV; ++x) s += ws[x];
   const float l = (zy - m) / a.tau - logf(s);
   const float ratio = a.old != nullptr ? expf(l - a.old[row]) : 1.0f;
-  const float whole = ratio * A;
+  const float whole = A == 0.0f && ratio == INFINITY ? 0.0f : ratio * A;         // 0 whatever the ratio, not 0 times infinity
   const float cut = (ratio < 1.0f - a.low ? 1.0f - a.low : ratio > 1.0f + a.high ? 1.0f + a.high : ratio) * A;
   float loss = whole > cut ? -cut : -whole, c = whole > cut ? 0.0f : -whole;       // NaN stays NaN
   if (a.kl != 0.0f) {
