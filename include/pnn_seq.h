@@ -224,7 +224,8 @@ typedef struct {
  *     a = post ? w_post norm(x) : x,   h = res + alpha a silu(gate),   y = w_pre norm(h)   (pre != 0)
  * w_post, w_pre: float[width], the same for every head (NULL: ones).  gate, res (NULL: without), h (NULL: not wanted,
  * with pre; may be res itself, with the same strides: the backward then takes it with `stored`), y (needed if pre != 0, not looked at otherwise).  y is formed from the sum
- * before it is rounded to h.  silu(-inf) is 0.  A row whose squares pass the float range is normed to zeros. */
+ * before it is rounded to h.  silu(-inf) is 0.  A row whose squares pass the float range is normed to zeros,
+ * with no gradient through that norm. */
 pnn_status pnn_norm_fwd(const pnn_norm_desc* d, const void* x, const float* w_post, const void* gate, const void* res,
                         const float* w_pre, void* h, void* y, void* stream);
 

@@ -194,6 +194,8 @@ __device__ __forceinline__ float silu_slope(float g, float s) {
   return s == 0.0f ? 0.0f : s == 1.0f ? 1.0f : s * fmaf(g, 1.0f - s, 1.0f);
 }
 __device__ __forceinline__ float inverse_root(float mean, float eps) { return 1.0f / sqrtf(mean + eps); }
+// r^2 mean(t u); 0 for a row that is normed to zeros, whose sum may be infinite
+__device__ __forceinline__ float mean_part(float mean, float r) { return r == 0.0f ? 0.0f : mean * r * r; }
 
 template <typename T, int TL, int NP, bool TAIL>
 __global__ __launch_bounds__(TL < 256 ? 256 : TL) void norm_fwd_kernel(Norm a) {
@@ -325,7 +327,7 @@ __global__ __launch_bounds__(TL < 256 ? 256 : TL, norm_waves(TL, NP * St<T>::VE,
         s[1] = fmaf(t[e] * w[e], h[e], s[1]);
       }
       row_sums<TL, 2>(s, lds2, flip2);
-      const float r2 = inverse_root(s[0] * a.inv_width, a.eps), m2 = s[1] * a.inv_width * r2 * r2;
+      const float r2 = inverse_root(s[0] * a.inv_width, a.eps), m2 = mean_part(s[1] * a.inv_width, r2);
 #pragma unroll
       for (int e = 0; e < N; ++e) {
         d[e] = fmaf(r2, fmaf(-h[e], m2, t[e] * w[e]), d[e]);
@@ -354,7 +356,7 @@ __global__ __launch_bounds__(TL < 256 ? 256 : TL, norm_waves(TL, NP * St<T>::VE,
         m[0] = fmaf(d[e], x[e], m[0]);
       }
       row_sums<TL, 1>(m, lds1, flip1);
-      const float m1 = m[0] * a.inv_width * r1 * r1;
+      const float m1 = mean_part(m[0] * a.inv_width, r1);
 #pragma unroll
       for (int e = 0; e < N; ++e) d[e] = r1 * fmaf(-x[e], m1, d[e]);
     }
