@@ -1,6 +1,8 @@
 // Entry points of the sequence operators (pnn_seq.h): argument checks, then the launchers.
 #include <math.h>
 
+#include <initializer_list>
+
 #include "pnn_seq.h"
 #include "seq_internal.h"
 
@@ -14,6 +16,18 @@ constexpr int64_t MAX_SPAN = int64_t(1) << 60;
 bool type_ok(int t) { return t == PNN_F32 || t == PNN_BF16; }
 int type_size(int t) { return t == PNN_F32 ? 4 : 2; }
 bool aligned(const void* p, uintptr_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
+
+// whether an output starts where another one or an input does; NULL: a tensor that the call does not look at
+bool meet(std::initializer_list<const void*> out, std::initializer_list<const void*> in) {
+  for (auto o = out.begin(); o != out.end(); ++o) {
+    if (*o == nullptr) continue;
+    for (auto p = o + 1; p != out.end(); ++p)
+      if (*p == *o) return true;
+    for (const void* p : in)
+      if (p == *o) return true;
+  }
+  return false;
+}
 
 // elements from the first to the last of `rows` rows of `width`, `stride` apart; < 0: too many
 int64_t span(int64_t rows, int64_t stride, int64_t width) {
@@ -290,7 +304,9 @@ pnn_status pnn_linattn_fwd(const pnn_linattn_desc* d, const void* q, const void*
   if (!aligned(q, es) || !aligned(k, es) || !aligned(v, es) || !aligned(o, es) || !aligned(log_decay, 4) ||
       !aligned(lengths, 4) || !aligned(s0, 4) || !aligned(sT, 4) || !aligned(workspace, 256))
     return PNN_ERR_ALIGN;
-  if (d->length > 0 && (o == q || o == k || o == v)) return PNN_ERR_SHAPE;
+  if (d->length == 0) q = k = v = nullptr, o = nullptr;
+  const void* const ws = lin_fwd_bytes(*d) > 0 ? workspace : nullptr;
+  if (meet({o, sT}, {q, k, v, log_decay, lengths, ws}) || meet({o}, {s0})) return PNN_ERR_SHAPE;
   return launch_linattn_fwd(*d, q, k, v, log_decay, lengths, s0, o, sT, workspace, (hipStream_t)stream) ? PNN_ERR_HIP
                                                                                                         : PNN_OK;
 }
@@ -316,15 +332,9 @@ pnn_status pnn_linattn_bwd(const pnn_linattn_desc* d, const void* q, const void*
       !aligned(dk, es) || !aligned(dv, es) || !aligned(log_decay, 4) || !aligned(lengths, 4) || !aligned(s0, 4) ||
       !aligned(dsT, 4) || !aligned(ds0, 4) || !aligned(workspace, 256))
     return PNN_ERR_ALIGN;
-  if (ds0 != nullptr && (ds0 == dsT || ds0 == s0)) return PNN_ERR_SHAPE;
-  if (d->length > 0) {
-    const void *in[4] = {q, k, v, dout}, *out[3] = {dq, dk, dv};
-    for (int i = 0; i < 3; ++i) {
-      if (out[i] == out[(i + 1) % 3]) return PNN_ERR_SHAPE;
-      for (int j = 0; j < 4; ++j)
-        if (out[i] == in[j]) return PNN_ERR_SHAPE;
-    }
-  }
+  if (d->length == 0) q = k = v = dout = nullptr, dq = dk = dv = nullptr;
+  const void* const ws = lin_bwd(*d).bytes > 0 ? workspace : nullptr;
+  if (meet({dq, dk, dv, ds0}, {q, k, v, dout, log_decay, lengths, s0, dsT, ws})) return PNN_ERR_SHAPE;
   return launch_linattn_bwd(*d, q, k, v, log_decay, lengths, s0, dout, dsT, dq, dk, dv, ds0, workspace,
                             (hipStream_t)stream)
              ? PNN_ERR_HIP
@@ -350,8 +360,7 @@ pnn_status pnn_norm_fwd(const pnn_norm_desc* d, const void* x, const float* w_po
   if (!aligned(x, es) || !aligned(w_post, 4) || !aligned(gate, es) || !aligned(res, es) || !aligned(w_pre, 4) ||
       !aligned(h, es) || !aligned(y, es))
     return PNN_ERR_ALIGN;
-  if (h != nullptr && (h == x || h == gate || h == y)) return PNN_ERR_SHAPE;
-  if (y != nullptr && (y == x || y == gate || y == res)) return PNN_ERR_SHAPE;
+  if (meet({h, y}, {x, gate, d->post ? w_post : nullptr, d->pre ? w_pre : nullptr}) || meet({y}, {res})) return PNN_ERR_SHAPE;
   if (h != nullptr && h == res && !same(d->h, d->res, d)) return PNN_ERR_SHAPE;
   return launch_norm_fwd(*d, x, w_post, gate, res, w_pre, h, y, (hipStream_t)stream) ? PNN_ERR_HIP : PNN_OK;
 }
@@ -391,13 +400,10 @@ pnn_status pnn_norm_bwd(const pnn_norm_desc* d, const void* x, const float* w_po
   if (!aligned(w_post, 4) || !aligned(w_pre, 4) || !aligned(dw_post, 4) || !aligned(dw_pre, 4) ||
       !aligned(workspace, 256))
     return PNN_ERR_ALIGN;
-  for (int i = 5; i < 8; ++i)
-    for (int j = 0; j < i; ++j)
-      if (tensors[i].p != nullptr && tensors[i].p == tensors[j].p && !(i == 7 && j == 4 && same(d->dres, d->dh, d)))
-        return PNN_ERR_SHAPE;
-  const float* const dw[2] = {dw_post, dw_pre};
-  for (int i = 0; i < 2; ++i)
-    if (dw[i] != nullptr && (dw[i] == dw[1 - i] || dw[i] == w_post || dw[i] == w_pre)) return PNN_ERR_SHAPE;
+  const void* const ws = dw_post != nullptr || dw_pre != nullptr ? workspace : nullptr;
+  if (meet({dx, dgate, dres, dw_post, dw_pre}, {x, gate, res, dy, w_post, w_pre, ws}) ||
+      meet({dx, dgate, dw_post, dw_pre}, {dh}) || (dres != nullptr && dres == dh && !same(d->dres, d->dh, d)))
+    return PNN_ERR_SHAPE;
   return launch_norm_bwd(*d, x, w_post, gate, res, w_pre, dy, dh, dx, dgate, dres, dw_post, dw_pre, accumulate, workspace,
                          (hipStream_t)stream)
              ? PNN_ERR_HIP
@@ -428,9 +434,7 @@ pnn_status pnn_policy_fwd_bwd(const pnn_policy_desc* d, const void* logits, cons
       !aligned(old, 4) || !aligned(ref, 4) || !aligned(weight, 4) || !aligned(loss, 4) || !aligned(logp, 4))
     return PNN_ERR_ALIGN;
   if (dlogits == logits && d->rows > 1 && d->grad_stride != d->logit_stride) return PNN_ERR_SHAPE;
-  if (loss == logp) return PNN_ERR_SHAPE;
-  for (const float* in : {advantage, old, ref, weight})
-    if (in != nullptr && (loss == in || logp == in)) return PNN_ERR_SHAPE;
+  if (meet({loss, logp, dlogits}, {tokens, advantage, old, ref, weight}) || meet({loss, logp}, {logits})) return PNN_ERR_SHAPE;
   return launch_policy(*d, logits, tokens, advantage, old, ref, weight, loss, logp, dlogits, (hipStream_t)stream)
              ? PNN_ERR_HIP
              : PNN_OK;
