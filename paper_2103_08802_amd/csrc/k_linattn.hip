@@ -26,9 +26,11 @@
 // operands read ahead, more registers and fewer waves: no gain (107, backward 166), spills in the eight-wave form.
 //
 // Roundings to bf16 besides the outputs' (bf16 tensors only): the weighted q k and the state, where they are operands
-// of the products with v and q; each is as large as the output's own rounding.  The state itself is fp32, and the
-// weighted values that are added to it are split into two bf16 parts (16 bits), and three (24 bits) where the caller
-// wants the state.
+// of the products with v and q; together they are as large as the output's own rounding (outputs 2.34e-3 from 64 bits;
+// two bf16 parts of each 1.66e-3, the output's rounding alone, but the training batch 315 us for 268 and the prompt 235 for
+// 217).  The state itself is fp32, and the weighted values that are added to it are split into two bf16 parts: 16 bits,
+// under a hundredth of the state's rounding as an operand, which is all that a call without sT (ds0) reads it for, its
+// segments' states and the sums of dk and dq included.  Three parts (24 bits) where the caller wants the state.
 #include "device_common.h"
 #include "seq_device.h"
 #include "seq_internal.h"

@@ -9,10 +9,10 @@
 // a row has more than a wave.
 //
 // Bound by memory.  bf16, 16384 rows of 2048 with a residual: forward 52 us (269 MB, 5.1 TB/s), backward 85 us (424 MB,
-// 5.0 TB/s, 21 MB of it partial weight gradients) and 8.5 us to join these.  262144 heads of 128 with a gate: forward 38
-// us (201 MB, 5.3 TB/s), backward 58 us (336 MB, 5.8 TB/s) and 5.  Rows are loaded when their turn comes: a row ahead in
-// registers costs a wave a SIMD and gained nothing.  Stores of tensors larger than L2 go past it (heads' backward 107 us
-// if they do not).
+// 5.0 TB/s, 21 MB of it partial weight gradients) and 8.5 us to join these; one after the other the two take 95.7 us where
+// h is formed and 89.9 where it is read.  262144 heads of 128 with a gate: forward 38 us (201 MB, 5.3 TB/s), backward 58 us
+// (336 MB, 5.8 TB/s) and 5.  Rows are loaded when their turn comes: a row ahead in registers costs a wave a SIMD and gained
+// nothing.  Stores of tensors larger than L2 go past it (heads' backward 107 us if they do not).
 #include "device_common.h"
 #include "seq_device.h"
 #include "seq_internal.h"
@@ -73,7 +73,7 @@ struct Cols {
         r[p] = make_uint4(w[0], w[1], w[2], w[3]);
       }
     }
-    if constexpr (TAIL && !HELD) {               // 1024 lanes have no registers for that
+    if constexpr (TAIL && !HELD) {               // 1024 lanes have no registers for two pieces' (one: not measured)
       unpack(r, lane, width, v);
 #pragma unroll
       for (int e = 0; e < N; ++e) asm volatile("" : "+v"(v[e]));
